@@ -448,6 +448,124 @@ int vitint_fold_requant(float x_step, const float* w_step, const float* bias, co
 int vitint_fold_layernorm_references(const float* gamma, const float* beta, float step, int32_t bits,
                                      int32_t is_signed, int64_t cols, float* refs, uint8_t* flip);
 
+/* ---- a paged cache of keys and values, for attention of new tokens over earlier ones ------------------------------------
+ *
+ * A decoder keeps the keys and values of all earlier tokens.  They lie in pages of page_tokens places; token j of a
+ * sequence is in page page_table[sequence][j / page_tokens], place j % page_tokens.  An element (page p, head h, place t,
+ * channel c) of keys or values is at p*page_stride + h*head_stride + t*token_stride + c (elements).
+ *
+ * Values are 16-bit, or signed 8-bit codes with one step for each token and head.  As in the linears the integers enter
+ * the contraction and their steps are applied behind it (Section III): a score is scale * k_step[j] * (q . k_code[j]), an
+ * output sum_j (p_j * v_step[j]) * v_code[j].
+ */
+typedef enum { VITINT_F32 = 0, VITINT_BF16 = 1, VITINT_F16 = 2, VITINT_I8 = 3 } vitint_dtype;
+
+typedef struct {
+    void* k;                 /* device, 16-byte aligned */
+    void* v;                 /* same type, sizes and strides as k */
+    float* k_steps;          /* VITINT_I8: device [pages][kv_heads][page_tokens], 16-byte aligned; NULL otherwise */
+    float* v_steps;
+    int64_t pages;
+    int64_t page_stride, head_stride, token_stride; /* elements; each a multiple of 16 bytes */
+    int32_t kv_heads;
+    int32_t page_tokens;     /* 16, 32, 64 or 128 */
+    int32_t head_dim;        /* 64 or 128 */
+    int32_t type;            /* VITINT_BF16, VITINT_F16 or VITINT_I8 */
+} vitint_cache;
+
+/* The sequences of one call.  lengths and query_starts are read on the device, so a recorded graph may be replayed with
+ * other contents; what the host declares (sequences, max_queries, max_length) bounds them and selects the kernels.
+ *   lengths[b]: tokens of sequence b in the cache, its new ones included (those are stored before the call);
+ *   query_starts[b] .. query_starts[b+1]: the rows of q that are the last tokens of sequence b (ascending, from row 0 on;
+ *     an empty range is allowed).  Rows behind query_starts[sequences] belong to no sequence and are left as they are. */
+typedef struct {
+    const int32_t* page_table;   /* device [sequences][table_stride]; entries behind a sequence's last page are not read */
+    int64_t table_stride;        /* entries of a row */
+    const int32_t* lengths;      /* device [sequences] */
+    const int32_t* query_starts; /* device [sequences + 1] */
+    int32_t sequences;
+    int32_t max_queries;         /* no sequence has more new tokens */
+    int64_t max_length;          /* no sequence is longer; at most table_stride * page_tokens and 2^30 */
+} vitint_cache_batch;
+
+/* Norm of every query and key head, rotation by the token's position, and the store of keys and values in the cache, in one
+ *   pass over the rows of a QKV projection.  For each head row x of head_dim channels, in fp32:
+ *     norm RMS:   y = x / sqrt(mean(x^2) + eps) * gain;   LAYER: y = (x - mean) / sqrt(var + eps) * gain + offset;   NONE: y = x
+ *     rotation of the first `rotary` channels by the angles a_i = position * frequencies[i], i < rotary/2, the product and its
+ *     reduction to one turn in fp64: the pair (y1, y2) becomes (y1 cos a_i - y2 sin a_i, y2 cos a_i + y1 sin a_i).  pairs == 0:
+ *     channels i and i + rotary/2; pairs == 1: channels 2i and 2i + 1.  Values (v) are neither normed nor rotated.
+ *   Results are rounded once: to out_type in q_out and k_out, to the cache's type in the cache; codes take the step
+ *   max|y| / 127 of their head row and q = rint(y / step) (a row of zeros has step 0 and codes 0).
+ *   q: [tokens, q_heads*head_dim] of in_type (VITINT_F32, BF16, F16), rows q_stride elements apart; k, v: [tokens, kv_heads*head_dim]
+ *     with k_stride, v_stride.  Pointers and strides in bytes are multiples of 16.  q may be NULL with q_heads 0.
+ *   gains, offsets: device fp32 [head_dim] (offsets for LAYER only, NULL otherwise; gains NULL for NONE).
+ *   positions: device int32 [tokens], frequencies: device fp64 [rotary/2] (both may be NULL if rotary is 0); rotary is a
+ *     multiple of 16, at most head_dim.
+ *   q_out: [tokens, q_heads, head_dim] of out_type (VITINT_BF16, F16), contiguous heads, rows q_out_stride elements apart; may be q itself (same type).
+ *   k_out: the same for keys, or NULL.
+ *   cache, slots: device int64 [tokens], the place page*page_tokens + t that token t's key and value go to; a negative slot
+ *     stores nothing, and neither does one behind the last page.  Two tokens never share a slot.  cache may be NULL
+ *     (then v, slots and weights are NULL too and k_out is needed).  weights: device fp32 [pages][kv_heads][page_tokens] or NULL:
+ *     the accumulated weight of every stored place is set to 0.
+ *   Errors: INVALID_ARG, UNSUPPORTED (head_dim, rotary), ALIGNMENT, CUDA. */
+typedef enum { VITINT_NORM_NONE = 0, VITINT_NORM_RMS = 1, VITINT_NORM_LAYER = 2 } vitint_head_norm;
+typedef struct {
+    const void *q, *k, *v;
+    int64_t tokens, q_stride, k_stride, v_stride;
+    int32_t q_heads, kv_heads, head_dim, in_type;
+    int32_t norm;                /* vitint_head_norm */
+    float eps;
+    const float *q_gain, *k_gain, *q_offset, *k_offset;
+    const int32_t* positions;
+    const double* frequencies;
+    int32_t rotary, pairs;
+    void *q_out, *k_out;
+    int64_t q_out_stride, k_out_stride;
+    int32_t out_type;
+    int32_t reserved_;           /* set to 0 */
+    const int64_t* slots;
+    float* weights;
+} vitint_qk_norm_rotate_desc;
+int vitint_qk_norm_rotate(const vitint_qk_norm_rotate_desc* d, const vitint_cache* cache, void* stream);
+
+/* Attention of every sequence's new tokens over what the cache holds of it (Eq. 3 for new tokens).  Query i of a sequence with
+ *   n new tokens and length L has position L - n + i; it sees key j < L where causal == 0, j <= position where causal == 1 and,
+ *   with window > 0 (causal only), j > position - window.  Scores and the softmax's maximum and sum are fp32; probabilities
+ *   enter the second contraction rounded to the queries' type.  A query that sees no key gives zeros and lse = -inf.
+ *   q: [tokens, q_heads, head_dim] of q_type (VITINT_BF16 or F16; the cache's type unless that is VITINT_I8), channel stride 1,
+ *     16-byte aligned, strides multiples of 8 elements.  q_heads is a multiple of kv_heads: query head h reads
+ *     head h / (q_heads / kv_heads); at most 128 query heads share one.  out: same type and rules.
+ *   lse: device fp32 [tokens, q_heads], the logarithm of each row's sum of exponentials of scaled scores, or NULL.
+ *   What the cache's pages hold behind a sequence's length is never used, whatever it is.  Within the length keys and values
+ *   are finite: a value that is not may reach queries that the mask keeps from it.
+ *   workspace: device scratch, 256-byte aligned, >= vitint_paged_attention_workspace_bytes(); contents undefined after; two calls
+ *     that may overlap (streams, graphs replayed side by side) need one each.
+ *   A page index outside the cache reads as zeros, a length beyond max_length or page table counts as that bound, and query ranges
+ *     outside q are cut; each makes the next vitint_device_status() return VITINT_ERR_INVALID_ARG.
+ *   Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
+size_t vitint_paged_attention_workspace_bytes(int32_t q_heads, const vitint_cache* cache, const vitint_cache_batch* batch);
+int vitint_paged_attention(const void* q, int32_t q_type, int64_t tokens, int32_t q_heads, int64_t q_token_stride,
+                           int64_t q_head_stride, const vitint_cache* cache, const vitint_cache_batch* batch, float scale,
+                           int32_t causal, int32_t window, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                           float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated weight.  Of each sequence and head of the cache the first `sinks` tokens, the last `recent` ones and, of
+ *   the others, those of largest weight are kept, `budget` in all (all of a sequence that has no more); equal weights go to the
+ *   lowest index.  Kept tokens stay in order.  Their keys, values, steps and weights are copied to the places 0, 1, ... of the pages that
+ *   new_table names; the pages they came from are not written (another sequence may share them).
+ *   weights: device fp32 [pages][kv_heads][page_tokens], read at the old places and written at the new ones; not NaN.
+ *   new_table: device int32 [sequences][new_table_stride], new_table_stride * page_tokens >= budget; its pages are none that
+ *     the batch's page table uses and none is named twice.
+ *   kept: device int32 [sequences][kv_heads][budget], the indices kept, -1 behind them.  counts: device int32 [sequences],
+ *     min(length, budget): the new lengths.  counts is not batch->lengths.
+ *   batch: query_starts and max_queries are not used.  sinks + recent <= budget.
+ *   Page indexes outside the cache, and lengths beyond the batch's bounds, are not followed and make the next
+ *     vitint_device_status() return VITINT_ERR_INVALID_ARG.
+ *   Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */
+int vitint_cache_evict(const vitint_cache* cache, const vitint_cache_batch* batch, float* weights, int32_t budget, int32_t sinks,
+                       int32_t recent, const int32_t* new_table, int64_t new_table_stride, int32_t* kept, int32_t* counts,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

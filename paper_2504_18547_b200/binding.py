@@ -132,6 +132,13 @@ def lib():
         L.vitint_fold_requant.argtypes = [c_float, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
         L.vitint_fold_layernorm_references.argtypes = [c_void_p, c_void_p, c_float, c_int32, c_int32, c_int64, c_void_p,
                                                        c_void_p]
+        L.vitint_qk_norm_rotate.argtypes = [c_char_p, c_char_p, c_void_p]
+        L.vitint_paged_attention_workspace_bytes.restype = c_size_t
+        L.vitint_paged_attention_workspace_bytes.argtypes = [c_int32, c_char_p, c_char_p]
+        L.vitint_paged_attention.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_int64, c_int64, c_char_p, c_char_p, c_float, c_int32,
+                                             c_int32, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.vitint_cache_evict.argtypes = [c_char_p, c_char_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
+                                         c_void_p]
         L.vitint_layernorm_quantize.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_float,
                                                 c_float, POINTER(_Codes), c_void_p, c_int64, c_void_p]
         _lib = L
@@ -623,3 +630,205 @@ def vitint_layernorm_compare_quantize(x: torch.Tensor, refs: torch.Tensor, flip:
                                                    float(n_eps), byref(d), stats.data_ptr(), _stream()),
            "vitint_layernorm_compare_quantize")
     return out, stats
+
+
+# ---------------------------------------------------------------------------
+# the paged cache
+# ---------------------------------------------------------------------------
+
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_I8 = range(4)
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.int8: DTYPE_I8}
+_NORMS = {"none": 0, "rms": 1, "layer": 2}
+_ERR_INVALID_ARG = -1
+# vitint_cache, vitint_cache_batch and vitint_qk_norm_rotate_desc, field by field: one packing call instead of a structure's constructor
+_PACK_CACHE = struct.Struct("@4P4q4i").pack
+_PACK_BATCH = struct.Struct("@PqPP2iq").pack
+_PACK_ROTATE = struct.Struct("@3P4q4iif4P2P2i2P2q2i2P").pack
+
+
+def _require(holds: bool, where: str, what: str) -> None:
+    if not holds:
+        raise VitintError(_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _here(where: str, *tensors) -> None:
+    """The call is made on the current device's stream: its tensors are there."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise VitintError(_ERR_INVALID_ARG, f"{where}: a tensor is not on the current device")
+
+
+def _array(t, where: str, name: str, dtype, shape) -> None:
+    """A contiguous tensor of exactly this type and shape."""
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise VitintError(_ERR_INVALID_ARG, f"{where}: {name} is a contiguous {dtype} tensor {list(shape)}")
+
+
+@dataclass
+class PagedCache:
+    """Keys and values [pages, kv_heads, page_tokens, head_dim] of earlier tokens (bf16, fp16, or int8 codes with fp32 steps
+    [pages, kv_heads, page_tokens]).  k and v may be views with equal strides (any order of pages, heads and places)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_steps: torch.Tensor | None = None
+    v_steps: torch.Tensor | None = None
+
+    @staticmethod
+    def empty(pages: int, kv_heads: int, page_tokens: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
+        shape = (pages, kv_heads, page_tokens, head_dim)
+        kv = [torch.empty(shape, dtype=dtype, device=device) for _ in range(2)]
+        steps = [torch.empty(shape[:3], device=device) if dtype == torch.int8 else None for _ in range(2)]
+        return PagedCache(*kv, *steps)
+
+    def desc(self, where: str = "PagedCache") -> bytes:
+        k, v, ks, vs = self.k, self.v, self.k_steps, self.v_steps
+        pages, heads, places, dim = k.shape
+        stride = k.stride()
+        kind = _DTYPES.get(k.dtype, DTYPE_F32)
+        _require(kind != DTYPE_F32 and v.dtype == k.dtype and v.shape == k.shape and v.stride() == stride and stride[3] == 1, where,
+                 "k and v have one type (bf16, fp16, int8), shape and strides, channels last")
+        if kind == DTYPE_I8:
+            _require(ks is not None and vs is not None, where, "codes come with steps")
+            _array(ks, where, "k_steps", torch.float32, (pages, heads, places))
+            _array(vs, where, "v_steps", torch.float32, (pages, heads, places))
+        else:
+            _require(ks is None and vs is None, where, "16-bit values have no steps")
+        return _PACK_CACHE(k.data_ptr(), v.data_ptr(), _ptr(ks) or 0, _ptr(vs) or 0, pages, stride[0], stride[1], stride[2], heads, places, dim, kind)
+
+
+@dataclass
+class CacheBatch:
+    """The sequences of a call: page_table [sequences, entries], lengths [sequences] (new tokens included), query_starts
+    [sequences + 1] (rows of each sequence's new tokens), all int32 on the device, and the host's bounds on them."""
+    page_table: torch.Tensor
+    lengths: torch.Tensor
+    query_starts: torch.Tensor | None
+    max_queries: int
+    max_length: int
+
+    def desc(self, where: str = "CacheBatch") -> bytes:
+        table, lengths, starts = self.page_table, self.lengths, self.query_starts
+        n = lengths.shape[0]
+        _require(table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1, where,
+                 "page_table is an int32 tensor [sequences, entries]")
+        _array(lengths, where, "lengths", torch.int32, (n,))
+        if starts is not None:
+            _array(starts, where, "query_starts", torch.int32, (n + 1,))
+        stride = table.stride(0) if n > 1 else table.shape[1]
+        _require(self.max_length <= table.shape[1] << 30, where, "max_length fits the page table")
+        return _PACK_BATCH(table.data_ptr(), stride, lengths.data_ptr(), _ptr(starts) or 0, n, self.max_queries, self.max_length)
+
+
+def vitint_qk_norm_rotate(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor | None, head_dim: int, norm: str = "rms", eps: float = 1e-6,
+                          q_gain: torch.Tensor | None = None, k_gain: torch.Tensor | None = None, q_offset: torch.Tensor | None = None,
+                          k_offset: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                          frequencies: torch.Tensor | None = None, pairs: bool = False, q_out: torch.Tensor | None = None,
+                          k_out: torch.Tensor | None = None, out_dtype=None, cache: PagedCache | None = None,
+                          slots: torch.Tensor | None = None, weights: torch.Tensor | None = None):
+    """Norm of every query and key head, rotation by position and the store of keys and values in the cache.  q, k, v: 2-D rows
+    [tokens, heads * head_dim] (slices of one projection's output may be given).  Rotates the first 2 * len(frequencies) channels.
+    Returns (q_out [tokens, q_heads, head_dim], k_out: given, or made where there is no cache)."""
+    where = "vitint_qk_norm_rotate"
+    tokens, in_type = k.shape[0], _DTYPES.get(k.dtype, DTYPE_I8)
+    rows = [t for t in (q, k, v) if t is not None]
+    for t in rows:
+        _require(t.dim() == 2 and t.shape[0] == tokens and t.dtype == k.dtype and t.stride(1) == 1 and t.shape[1] % head_dim == 0, where,
+                 "q, k and v are rows [tokens, heads * head_dim] of one type")
+    _require(in_type != DTYPE_I8 and norm in _NORMS, where, "rows are fp32, bf16 or fp16, the norm is none, rms or layer")
+    _require((v is None) == (cache is None) and (slots is None) == (cache is None) and (v is None or v.shape[1] == k.shape[1]), where,
+             "v and slots come with a cache")
+    if out_dtype is None:
+        out_dtype = next((t.dtype for t in (q_out, k_out) if t is not None), None) or (
+            cache.k.dtype if cache is not None and cache.k.dtype != torch.int8 else k.dtype if k.dtype != torch.float32 else torch.bfloat16)
+    hq, hk = 0 if q is None else q.shape[1] // head_dim, k.shape[1] // head_dim
+    if q is not None and q_out is None:
+        q_out = torch.empty((tokens, hq, head_dim), dtype=out_dtype, device=k.device)
+    if cache is None and k_out is None:
+        k_out = torch.empty((tokens, hk, head_dim), dtype=out_dtype, device=k.device)
+    for t, heads in ((q_out, hq), (k_out, hk)):
+        if t is not None:
+            _require(t.dtype == out_dtype and tuple(t.shape) == (tokens, heads, head_dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim),
+                     where, "q_out and k_out are [tokens, heads, head_dim] of one 16-bit type, heads behind one another")
+    for name, t in (("q_gain", q_gain), ("k_gain", k_gain), ("q_offset", q_offset), ("k_offset", k_offset)):
+        if t is not None:
+            _array(t, where, name, torch.float32, (head_dim,))
+    if frequencies is not None:
+        _array(frequencies, where, "frequencies", torch.float64, (frequencies.shape[0],))
+        _require(positions is not None, where, "frequencies come with positions")
+        _array(positions, where, "positions", torch.int32, (tokens,))
+    dc = None
+    if cache is not None:
+        _array(slots, where, "slots", torch.int64, (tokens,))
+        if weights is not None:
+            _array(weights, where, "weights", torch.float32, tuple(cache.k.shape[:3]))
+        dc = cache.desc(where)
+    _here(where, *rows, q_out, k_out, q_gain, k_gain, q_offset, k_offset, positions, frequencies, slots, weights,
+          *(() if cache is None else (cache.k, cache.v, cache.k_steps, cache.v_steps)))
+    rotary = 0 if frequencies is None else 2 * frequencies.shape[0]
+    d = _PACK_ROTATE(_ptr(q) or 0, k.data_ptr(), _ptr(v) or 0, tokens, 0 if q is None else _ld(q), _ld(k), 0 if v is None else _ld(v),
+                     hq, hk, head_dim, in_type, _NORMS[norm], eps, _ptr(q_gain) or 0, _ptr(k_gain) or 0, _ptr(q_offset) or 0, _ptr(k_offset) or 0,
+                     (_ptr(positions) or 0) if rotary else 0, (_ptr(frequencies) or 0) if rotary else 0, rotary, int(bool(pairs)),
+                     _ptr(q_out) or 0, _ptr(k_out) or 0, 0 if q_out is None else max(q_out.stride(0), hq * head_dim if tokens == 1 else 0),
+                     0 if k_out is None else max(k_out.stride(0), hk * head_dim if tokens == 1 else 0), _DTYPES.get(out_dtype, DTYPE_F32), 0,
+                     _ptr(slots) or 0, _ptr(weights) or 0)
+    _check(lib().vitint_qk_norm_rotate(d, dc, _stream()), where)
+    return q_out, k_out
+
+
+def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, where: str):
+    _require(q.dim() == 3 and q.shape[2] == cache.k.shape[3] and q.stride(2) == 1, where, "q is [tokens, q_heads, head_dim], channels last")
+    _require(batch.query_starts is not None, where, "the batch names the queries' rows")
+    _here(where, q, cache.k, cache.v, cache.k_steps, cache.v_steps, batch.page_table, batch.lengths, batch.query_starts)
+    return _DTYPES.get(q.dtype, DTYPE_F32)
+
+
+def vitint_paged_attention_workspace_bytes(q_heads: int, cache: PagedCache, batch: CacheBatch) -> int:
+    return int(lib().vitint_paged_attention_workspace_bytes(q_heads, cache.desc(), batch.desc()))
+
+
+def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, scale: float, causal: bool = True, window: int = 0,
+                           out: torch.Tensor | None = None, lse: torch.Tensor | None = None, want_lse: bool = False,
+                           workspace: torch.Tensor | None = None):
+    """Attention of every sequence's new tokens (rows of q [tokens, q_heads, head_dim]) over what the cache holds of it.  Returns
+    out, or (out, lse [tokens, q_heads]) where lse is given or wanted."""
+    where = "vitint_paged_attention"
+    kind = _queries(q, cache, batch, where)
+    tokens, heads = q.shape[0], q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _require(out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1, where, "out has the shape and type of q, channels last")
+    if lse is None and want_lse:
+        lse = torch.empty((tokens, heads), device=q.device)
+    if lse is not None:
+        _array(lse, where, "lse", torch.float32, (tokens, heads))
+    dc, db = cache.desc(where), batch.desc(where)
+    if workspace is None:
+        workspace = torch.empty(lib().vitint_paged_attention_workspace_bytes(heads, dc, db), dtype=torch.uint8, device=q.device)
+    _here(where, out, lse, workspace)
+    qs, os = q.stride(), out.stride()
+    _check(lib().vitint_paged_attention(q.data_ptr(), kind, tokens, heads, qs[0], qs[1], dc, db, scale, int(bool(causal)), window, out.data_ptr(),
+                                        os[0], os[1], _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream()), where)
+    return out if lse is None else (out, lse)
+
+
+def vitint_cache_evict(cache: PagedCache, batch: CacheBatch, weights: torch.Tensor, budget: int, new_table: torch.Tensor, sinks: int = 0,
+                       recent: int = 0, kept: torch.Tensor | None = None, counts: torch.Tensor | None = None):
+    """Keeps `budget` tokens of every sequence and head (the first `sinks`, the last `recent`, of the others those of largest weight)
+    and copies them to the pages of new_table.  Returns (kept [sequences, kv_heads, budget], counts [sequences])."""
+    where = "vitint_cache_evict"
+    n, heads = batch.lengths.shape[0], cache.k.shape[1]
+    _require(budget > 0, where, "a budget of at least one token")
+    _array(weights, where, "weights", torch.float32, tuple(cache.k.shape[:3]))
+    _require(new_table.dtype == torch.int32 and new_table.dim() == 2 and new_table.shape[0] == n and new_table.stride(1) == 1, where,
+             "new_table is an int32 tensor [sequences, entries]")
+    if kept is None:
+        kept = torch.empty((n, heads, budget), dtype=torch.int32, device=weights.device)
+    if counts is None:
+        counts = torch.empty(n, dtype=torch.int32, device=weights.device)
+    _array(kept, where, "kept", torch.int32, (n, heads, budget))
+    _array(counts, where, "counts", torch.int32, (n,))
+    _here(where, cache.k, cache.v, cache.k_steps, cache.v_steps, batch.page_table, batch.lengths, weights, new_table, kept, counts)
+    _check(lib().vitint_cache_evict(cache.desc(where), batch.desc(where), weights.data_ptr(), budget, sinks, recent, new_table.data_ptr(),
+                                    new_table.stride(0) if n > 1 else new_table.shape[1], kept.data_ptr(), counts.data_ptr(), _stream()), where)
+    return kept, counts

@@ -62,11 +62,6 @@ extern "C" int64_t vitint_packed_pitch(int64_t cols, int32_t bits) {
 
 extern "C" int vitint_device_status(void) {
     if (cudaDeviceSynchronize() != cudaSuccess) return VITINT_ERR_CUDA;
-    int h = 0;
-    if (cudaMemcpyFromSymbol(&h, g_device_status, sizeof(int)) != cudaSuccess) return VITINT_ERR_CUDA;
-    if (h != 0) {
-        int zero = 0;
-        cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
-    }
-    return h;
+    const int h = take_status_word(), c = take_cache_status_word();
+    return h != 0 ? h : c;
 }

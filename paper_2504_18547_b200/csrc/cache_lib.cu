@@ -1,0 +1,6 @@
+// The paged cache and its operators as a translation unit of its own, compiled beside vitint_lib.cu.
+#include "qk_norm_rotate.cu"
+#include "cache_evict.cu"
+#include "paged_attention.cu"
+
+int vitint::take_cache_status_word() { return take_status_word(); }

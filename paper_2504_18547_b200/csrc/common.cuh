@@ -13,9 +13,21 @@
 
 namespace vitint {
 
-// Device status word: 0, or VITINT_ERR_TIMEOUT once any bounded wait gave up.  The library
-// is built as ONE translation unit (vitint_lib.cu), so this is the only instance.
-__device__ int g_device_status = 0;
+// Device status word: 0, or VITINT_ERR_TIMEOUT once any bounded wait gave up (or VITINT_ERR_INVALID_ARG, see
+// vitint_device_status).  One for each translation unit (vitint_lib.cu, cache_lib.cu); vitint_device_status() reads both.
+static __device__ int g_device_status = 0;
+
+// Reads and clears this unit's word.
+static inline int take_status_word() {
+    int h = 0;
+    if (cudaMemcpyFromSymbol(&h, g_device_status, sizeof(int)) != cudaSuccess) return VITINT_ERR_CUDA;
+    if (h != 0) {
+        int zero = 0;
+        cudaMemcpyToSymbol(g_device_status, &zero, sizeof(int));
+    }
+    return h;
+}
+int take_cache_status_word();          // that of cache_lib.cu
 
 inline int container_bits(int bits) { return bits == 3 ? 4 : bits; }
 inline bool valid_bits(int bits) { return bits == 2 || bits == 3 || bits == 4 || bits == 8; }

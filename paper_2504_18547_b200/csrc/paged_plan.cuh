@@ -1,0 +1,190 @@
+// How the attention kernels over the paged cache share their work out.
+//
+// An item is a head of the cache and a run of a sequence's new tokens (tile_tokens of them, all query heads of the group); its work
+// is a number of key tiles.  All items' key tiles, sequence by sequence, head by head, run by run, form one line, and every CTA
+// takes an equal stretch of it: whatever the lengths are, no CTA has more than one tile above the mean.  A stretch that ends inside
+// an item leaves a partial result (row maxima, sums and unnormalised outputs) in the workspace, at most two a CTA, and a second
+// kernel joins them.  The plan is made on the device from the lengths, so a recorded graph may be replayed with others; it is a
+// warp's work: lanes take sequences, or the runs of one long chunk.
+#pragma once
+
+#include "cache.cuh"
+
+namespace vitint {
+
+struct PlanParams {
+    SequenceView seq;
+    int kv_heads, group, tile_tokens;
+    int causal, window;                   // window 0: none
+};
+
+// Work of run p of a sequence: its first key (a multiple of KT) and its key tiles, at least one (a run that sees no key still
+// writes its rows).
+template <int KT>
+__device__ __forceinline__ int item_tiles(const PlanParams& A, const Sequence& s, int p, int& first_key) {
+    const int i0 = p * A.tile_tokens, i1 = min(s.queries, i0 + A.tile_tokens) - 1, base = s.length - s.queries;
+    const int end = A.causal ? min(base + i1 + 1, s.length) : s.length;
+    first_key = A.window ? max(base + i0 - A.window + 1, 0) / KT * KT : 0;
+    return max((end - first_key + KT - 1) / KT, 1);
+}
+__device__ __forceinline__ int runs_of(const PlanParams& A, const Sequence& s) { return (s.queries + A.tile_tokens - 1) / A.tile_tokens; }
+
+// Key tiles of one head of sequence `b` of every lane (0 where b is none).  Whole-warp.
+template <int KT>
+__device__ __forceinline__ int sequence_tiles(const PlanParams& A, int b, bool& ok) {
+    Sequence s{};
+    if (b < A.seq.sequences) s = sequence_of(A.seq, b, ok);
+    const int runs = runs_of(A, s);
+    int sum = 0, key;
+    if (runs <= 4)
+        for (int p = 0; p < runs; ++p) sum += item_tiles<KT>(A, s, p, key);
+    uint32_t many = __ballot_sync(0xffffffffu, runs > 4);
+    const int lane = threadIdx.x & 31;
+    while (many) {
+        const int from = __ffs(many) - 1;
+        many &= many - 1;
+        Sequence t;
+        t.length = __shfl_sync(0xffffffffu, s.length, from);
+        t.first = 0;
+        t.queries = __shfl_sync(0xffffffffu, s.queries, from);
+        int part = 0;
+        for (int p = lane; p < runs_of(A, t); p += 32) part += item_tiles<KT>(A, t, p, key);
+        part = __reduce_add_sync(0xffffffffu, part);
+        if (lane == from) sum = part;
+    }
+    return sum;
+}
+
+template <typename V>
+__device__ __forceinline__ V warp_inclusive_sum(V v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const V t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+// Where a CTA's stretch begins: item (b, h, p), the tile inside it, how many tiles follow, and (for the join) the first and
+// last CTA that work on that item.
+struct Stretch {
+    int b, h, p, tile;
+    int count;
+    int first_cta, last_cta;
+};
+
+// Whole-warp.  `bad`: whether the host's declarations do not hold.
+template <int KT>
+__device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, int ctas, bool& bad) {
+    const int lane = threadIdx.x & 31;
+    bool ok = true;
+    int total = 0;                                                     // (the host has checked that all tiles together fit)
+    const int first32 = sequence_tiles<KT>(A, lane, ok);               // kept: most calls have no more sequences
+    {
+        int sum = first32;
+        for (int b0 = 32; b0 < A.seq.sequences; b0 += 32) sum += sequence_tiles<KT>(A, b0 + lane, ok);
+        total = __reduce_add_sync(0xffffffffu, sum) * A.kv_heads;
+    }
+    bad = __any_sync(0xffffffffu, !ok);
+    const int per = max((total + ctas - 1) / ctas, 1);
+    Stretch r{};
+    const long long lo = (long long)cta * per;
+    if (lo >= total) return r;
+    r.count = min(per, total - (int)lo);
+    int base = 0;                                                      // tiles in front of the block of 32 sequences
+    for (int b0 = 0; b0 < A.seq.sequences; b0 += 32) {
+        const int t = b0 ? sequence_tiles<KT>(A, b0 + lane, ok) : first32;
+        const int all = t * A.kv_heads, sum = warp_inclusive_sum(all);
+        const uint32_t hit = __ballot_sync(0xffffffffu, base + sum > (int)lo);
+        if (!hit) {
+            base += __shfl_sync(0xffffffffu, sum, 31);
+            continue;
+        }
+        const int at = __ffs(hit) - 1;
+        const int tiles = __shfl_sync(0xffffffffu, t, at);
+        int begin = base + __shfl_sync(0xffffffffu, sum - all, at);    // first tile of the sequence
+        r.b = b0 + at;
+        r.h = ((int)lo - begin) / tiles;
+        begin += r.h * tiles;                                          // ... of its head
+        const Sequence s = sequence_of(A.seq, r.b);
+        const int runs = runs_of(A, s);
+        for (int p0 = 0;; p0 += 32) {
+            int key, n = 0;
+            if (p0 + lane < runs) n = item_tiles<KT>(A, s, p0 + lane, key);
+            const int psum = warp_inclusive_sum(n);
+            const uint32_t phit = __ballot_sync(0xffffffffu, begin + psum > (int)lo);
+            if (!phit) {
+                begin += __shfl_sync(0xffffffffu, psum, 31);
+                continue;
+            }
+            const int pat = __ffs(phit) - 1, size = __shfl_sync(0xffffffffu, n, pat);
+            begin += __shfl_sync(0xffffffffu, psum - n, pat);
+            r.p = p0 + pat;
+            r.tile = (int)lo - begin;
+            r.first_cta = begin / per;
+            r.last_cta = (begin + size - 1) / per;
+            return r;
+        }
+    }
+    r.count = 0;
+    return r;
+}
+
+// The items of a stretch, one after the other.
+template <int KT>
+struct StretchWalk {
+    int b, h, p, left;
+    int tile, end;             // this stretch's tiles of the item
+    int tiles, first_key;      // all of the item's tiles
+    Sequence s;
+    __device__ __forceinline__ void begin(const PlanParams& A, const Stretch& r) {
+        b = r.b; h = r.h; p = r.p; left = r.count; tile = r.tile;
+        if (left > 0) {
+            s = sequence_of(A.seq, b);
+            load(A);
+        }
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ void next(const PlanParams& A) {
+        left -= end - tile;
+        if (left <= 0) return;
+        tile = 0;
+        if (++p == runs_of(A, s)) {
+            p = 0;
+            if (++h == A.kv_heads) {
+                h = 0;
+                do s = sequence_of(A.seq, ++b); while (s.queries == 0);      // (another item follows: some sequence has it)
+            }
+        }
+        load(A);
+    }
+    __device__ __forceinline__ bool whole() const { return tile == 0 && end == tiles; }
+
+private:
+    __device__ __forceinline__ void load(const PlanParams& A) {
+        tiles = item_tiles<KT>(A, s, p, first_key);
+        end = min(tiles, tile + left);
+    }
+};
+
+// What a CTA whose stretch begins inside an item tells the join: the item and the CTAs that have parts of it.  Partial results lie
+// at slot 2c (CTA c began inside the item) and 2c + 1 (the item began in CTA c's stretch and did not end there).
+struct JoinNote {
+    int first_cta, last_cta;   // last_cta < 0: nothing to do
+    int b, h, p, pad_[3];
+};
+
+// Written by every CTA: the CTA behind an item's first one names it.
+__device__ __forceinline__ JoinNote join_note(const Stretch& r, int cta) {
+    JoinNote n{};
+    n.last_cta = -1;
+    if (r.count > 0 && r.tile > 0 && r.first_cta == cta - 1) {
+        n.first_cta = r.first_cta;
+        n.last_cta = r.last_cta;
+        n.b = r.b; n.h = r.h; n.p = r.p;
+    }
+    return n;
+}
+
+}  // namespace vitint

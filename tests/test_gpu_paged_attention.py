@@ -1,0 +1,202 @@
+"""Attention over the paged cache against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2504_18547_b200 as vt
+import paged_util as pu
+from gpu_util import GUARD_BYTES, check_guards, guarded_tensor
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, I8 = torch.bfloat16, torch.float16, torch.int8
+
+
+def run_case(seed, dim, places, qtype, ctype, kv_heads, group, seqs, causal=True, window=0, q_size=1.5, layout="hpd", spare=2, max_length=None):
+    """seqs: (cached tokens, new tokens) of each sequence."""
+    g = torch.Generator().manual_seed(seed)
+    lengths, news = [n for n, _ in seqs], [m for _, m in seqs]
+    pages = sum(-(-n // places) for n in lengths) + spare
+    cache = pu.random_cache(g, pages, kv_heads, places, dim, ctype, layout=layout)
+    table = pu.random_table(g, lengths, places, pages)
+    pu.spoil_unused(cache, table, lengths)
+    starts = torch.tensor([0] + news).cumsum(0).to(torch.int32)
+    tokens, heads = int(starts[-1]), kv_heads * group
+    q = (torch.randn(tokens + 3, heads, dim, generator=g) * q_size).to(qtype)       # three rows that belong to no sequence
+    scale = 1.0 / math.sqrt(dim)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), max(max(news), 1),
+                          max_length or max(max(lengths), 1))
+    out = guarded_tensor(q.shape, qtype)
+    lse = guarded_tensor(q.shape[:2], torch.float32)
+    out.fill_(7.0)
+    lse.fill_(7.0)
+    vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, scale, causal=causal, window=window, out=out, lse=lse)
+    assert vt.vitint_device_status() == 0
+    check_guards()
+    assert bool((out[tokens:] == 7.0).all()) and bool((lse[tokens:] == 7.0).all())
+    pu.check_attention(out, lse, pu.attention64(q, cache, table, lengths, starts, scale, causal, window))
+
+
+# few rows a head of the cache: one token or a few, every group size that fits sixteen rows
+@pytest.mark.parametrize("ctype,qtype", [(BF16, BF16), (F16, F16), (I8, BF16), (I8, F16)])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("places", [16, 32, 64, 128])
+def test_single_tokens(dim, places, ctype, qtype):
+    run_case(1, dim, places, qtype, ctype, 2, 4, [(1, 1), (15, 1), (16, 1), (17, 1), (129, 1), (300, 1), (63, 1)])
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+@pytest.mark.parametrize("group,new", [(1, 1), (1, 16), (2, 7), (3, 5), (5, 3), (6, 2), (7, 2), (8, 2), (12, 1), (16, 1)])
+def test_groups_and_drafts(group, new, ctype):
+    run_case(2, 64, 16, BF16, ctype, 3, group, [(97, new), (new, new), (211, 1)])
+
+
+def test_long_rows_are_split():
+    run_case(3, 128, 64, BF16, BF16, 2, 4, [(20001, 1), (3, 1), (7777, 1)])
+    run_case(4, 64, 16, F16, F16, 1, 1, [(30000, 2)])
+    run_case(5, 128, 32, F16, I8, 1, 8, [(16385, 2)])
+
+
+@pytest.mark.parametrize("ctype", [F16, I8])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 17), (True, 64), (True, 65), (True, 4000)])
+def test_masks(causal, window, ctype):
+    run_case(6, 64, 16, F16, ctype, 2, 3, [(200, 5), (64, 1), (130, 3), (5, 5)], causal, window)
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+def test_rows_without_keys(ctype):
+    """Sequences that are empty, shorter than their new tokens, or bring none."""
+    run_case(7, 128, 16, BF16, ctype, 2, 2, [(0, 2), (3, 5), (40, 0), (0, 0), (33, 2)])
+    run_case(8, 64, 32, BF16, ctype, 1, 2, [(0, 1)])
+
+
+def test_peaked_rows():
+    """Scores of hundreds: almost all weight on one key, and a maximum that keeps growing."""
+    run_case(9, 128, 16, BF16, BF16, 2, 4, [(700, 1), (333, 3)], q_size=60.0)
+    run_case(10, 128, 16, F16, I8, 2, 4, [(700, 1), (333, 3)], q_size=60.0)
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+def test_small_steps_and_layouts(ctype):
+    run_case(11, 128, 32, BF16, ctype, 4, 2, [(100, 2), (37, 1)], layout="phd")
+
+
+def test_tiny_value_steps_in_fp16():
+    """Steps far below fp16's range: the products are taken relative to the largest."""
+    g = torch.Generator().manual_seed(12)
+    cache = pu.random_cache(g, 20, 1, 16, 128, I8)
+    cache.v_steps.mul_(1e-4)
+    cache.v_steps[3:6].mul_(300.0)
+    table = pu.random_table(g, [300], 16, 20)
+    q = torch.randn(1, 4, 128, generator=g).to(F16)
+    starts = torch.tensor([0, 1], dtype=torch.int32)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor([300], dtype=torch.int32).cuda(), starts.cuda(), 1, 300)
+    out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.08, want_lse=True)
+    want = list(pu.attention64(q, cache, table, [300], starts, 0.08, True, 0))
+    want[2] += 2.0 ** -25                                  # outputs of 1e-3 and less: fp16's own subnormal step
+    pu.check_attention(out, lse, want)
+
+
+def _small(g, seqs=((90, 1), (200, 1)), dim=128, places=16, kv_heads=2, group=4, dtype=BF16, extra_pages=2, max_queries=None):
+    lengths, news = [n for n, _ in seqs], [m for _, m in seqs]
+    pages = sum(-(-n // places) for n in lengths) + extra_pages
+    cache = pu.random_cache(g, pages, kv_heads, places, dim, dtype)
+    table = pu.random_table(g, lengths, places, pages)
+    starts = torch.tensor([0] + news).cumsum(0).to(torch.int32)
+    q = torch.randn(int(starts[-1]), kv_heads * group, dim, generator=g).to(BF16)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), max_queries or max(news), max(lengths))
+    return cache, table, lengths, starts, q, batch
+
+
+@pytest.mark.parametrize("seqs", [((90, 1), (200, 1)), ((90, 30), (200, 77))])
+def test_strided_queries_and_outputs(seqs):
+    g = torch.Generator().manual_seed(20)
+    cache, table, lengths, starts, q, batch = _small(g, seqs)
+    fused = torch.zeros(q.shape[0], 3, 8 + 5, 128, dtype=BF16, device="cuda")        # queries inside wider rows
+    fused[:, 1, 2:10] = q.cuda()
+    wide = torch.full((q.shape[0], 20, 256), 3.0, dtype=BF16, device="cuda")
+    lse = torch.empty(q.shape[:2], device="cuda")
+    vt.vitint_paged_attention(fused[:, 1, 2:10], pu.to_gpu(cache), batch, 0.09, out=wide[:, 1:17:2, 128:], lse=lse)
+    pu.check_attention(wide[:, 1:17:2, 128:], lse, pu.attention64(q, cache, table, lengths, starts, 0.09, True, 0))
+    wide[:, 1:17:2, 128:] = 3.0
+    assert bool((wide == 3.0).all())
+
+
+@pytest.mark.parametrize("seqs", [((90, 1), (200, 1)), ((90, 30), (200, 77))])
+def test_recorded_call_replayed_with_other_lengths_on_another_stream(seqs):
+    g = torch.Generator().manual_seed(21)
+    cache, table, lengths, starts, q, batch = _small(g, seqs)
+    gpu, qd = pu.to_gpu(cache), q.cuda()
+    out, lse = torch.empty_like(qd), torch.empty(q.shape[:2], device="cuda")
+    workspace = torch.empty(vt.vitint_paged_attention_workspace_bytes(q.shape[1], gpu, batch), dtype=torch.uint8, device="cuda")
+    call = lambda: vt.vitint_paged_attention(qd, gpu, batch, 0.09, out=out, lse=lse, workspace=workspace)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+        for other in (lengths, [seqs[0][1], 131], [64, 199]):
+            batch.lengths.copy_(torch.tensor(other, dtype=torch.int32))
+            workspace.fill_(0x5A)
+            out.fill_(0)
+            graph.replay()
+            stream.synchronize()
+            pu.check_attention(out, lse, pu.attention64(q, cache, table, other, starts, 0.09, True, 0))
+    assert vt.vitint_device_status() == 0
+
+
+@pytest.mark.parametrize("seqs", [((9000, 1), (200, 1)), ((900, 30), (2000, 77))])
+def test_same_bits_every_time(seqs):
+    g = torch.Generator().manual_seed(22)
+    cache, *_, q, batch = _small(g, seqs)
+    gpu, qd = pu.to_gpu(cache), q.cuda()
+    first = [t.clone() for t in vt.vitint_paged_attention(qd, gpu, batch, 0.09, want_lse=True)]
+    for _ in range(5):
+        again = vt.vitint_paged_attention(qd, gpu, batch, 0.09, want_lse=True)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_bad_pages_and_lengths_are_reported(new):
+    """A page index outside the cache reads as zeros; lengths and ranges beyond the declared bounds are cut.  Nothing else is touched."""
+    g = torch.Generator().manual_seed(23)
+    cache, table, lengths, starts, q, batch = _small(g, ((200, new), (90, new)))
+    gpu, qd = pu.to_gpu(cache), q.cuda()
+    good = vt.vitint_paged_attention(qd, gpu, batch, 0.09).clone()
+    assert vt.vitint_device_status() == 0
+    bad = batch.page_table.clone()
+    bad[1, 2], bad[1, 3] = -5, 1 << 30
+    out = vt.vitint_paged_attention(qd, gpu, vt.CacheBatch(bad, batch.lengths, batch.query_starts, batch.max_queries, batch.max_length), 0.09)
+    assert vt.vitint_device_status() == -1 and vt.vitint_device_status() == 0
+    assert torch.equal(out[:new], good[:new])
+    long = torch.tensor([1 << 29, 90], dtype=torch.int32).cuda()
+    out = vt.vitint_paged_attention(qd, gpu, vt.CacheBatch(batch.page_table, long, batch.query_starts, batch.max_queries, batch.max_length), 0.09)
+    assert vt.vitint_device_status() == -1
+    assert torch.equal(out, good)                                                   # 2^29 counts as 200, the longest declared
+    ranges = torch.tensor([0, new, 100000], dtype=torch.int32).cuda()
+    out = vt.vitint_paged_attention(qd, gpu, vt.CacheBatch(batch.page_table, batch.lengths, ranges, batch.max_queries, batch.max_length), 0.09)
+    assert vt.vitint_device_status() == -1
+    assert torch.equal(out, good)
+    short = torch.tensor([0, -7, 2 * new], dtype=torch.int32).cuda()
+    vt.vitint_paged_attention(qd, gpu, vt.CacheBatch(batch.page_table, batch.lengths, short, batch.max_queries, batch.max_length), 0.09)
+    assert vt.vitint_device_status() == -1
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_offsets_beyond_32_bits(new):
+    """Pages that lie more than 2^32 bytes (2^31 elements) into the cache."""
+    g = torch.Generator().manual_seed(24)
+    places, dim, heads, pages = 128, 128, 2, (1 << 31) // (128 * 128 * 2) + 40
+    small = pu.random_cache(g, 8, heads, places, dim, BF16)
+    k, v = (torch.empty((pages, heads, places, dim), dtype=BF16, device="cuda") for _ in range(2))
+    at = torch.tensor([pages - 1, pages - 9, 0, 65536, pages - 3, pages - 4, 1, 2])
+    k[at.cuda()], v[at.cuda()] = small.k.cuda(), small.v.cuda()
+    order = torch.tensor([[0, 1, 2, 3, 4, 5, 6, 7]])
+    lengths, starts = [1000], torch.tensor([0, new], dtype=torch.int32)
+    q = torch.randn(new, 4, dim, generator=g).to(BF16)
+    batch = vt.CacheBatch(at[None].to(torch.int32).cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 1000)
+    out, lse = vt.vitint_paged_attention(q.cuda(), vt.PagedCache(k, v), batch, 0.09, want_lse=True)
+    pu.check_attention(out, lse, pu.attention64(q, small, order, lengths, starts, 0.09, True, 0))
