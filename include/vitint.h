@@ -485,7 +485,7 @@ typedef struct {
     const int32_t* query_starts; /* device [sequences + 1] */
     int32_t sequences;
     int32_t max_queries;         /* no sequence has more new tokens */
-    int64_t max_length;          /* no sequence is longer; at most table_stride * page_tokens and 2^30 */
+    int64_t max_length;          /* no sequence is longer; at most table_stride * page_tokens and 2^29 */
 } vitint_cache_batch;
 
 /* Norm of every query and key head, rotation by the token's position, and the store of keys and values in the cache, in one
@@ -506,7 +506,7 @@ typedef struct {
  *   cache, slots: device int64 [tokens], the place page*page_tokens + t that token t's key and value go to; a negative slot
  *     stores nothing, and neither does one behind the last page.  Two tokens never share a slot.  cache may be NULL
  *     (then v, slots and weights are NULL too and k_out is needed).  weights: device fp32 [pages][kv_heads][page_tokens] or NULL:
- *     the accumulated weight of every stored place is set to 0.
+ *     the accumulated weight (vitint_cache_weigh) of every stored place is set to 0.
  *   Errors: INVALID_ARG, UNSUPPORTED (head_dim, rotary), ALIGNMENT, CUDA. */
 typedef enum { VITINT_NORM_NONE = 0, VITINT_NORM_RMS = 1, VITINT_NORM_LAYER = 2 } vitint_head_norm;
 typedef struct {
@@ -548,6 +548,19 @@ int vitint_paged_attention(const void* q, int32_t q_type, int64_t tokens, int32_
                            int64_t q_head_stride, const vitint_cache* cache, const vitint_cache_batch* batch, float scale,
                            int32_t causal, int32_t window, void* out, int64_t out_token_stride, int64_t out_head_stride,
                            float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The attention weight that cached tokens receive: for every token j of every sequence and every head of the cache
+ *   weights_out[place of j] = weights_in[place of j] + sum over the new tokens i that see j and the query heads of the group
+ *                             of exp(score_ij - lse_i)
+ *   with the scores and the mask of vitint_paged_attention and the lse it returned.  Sums are fp32 in a fixed order.  Places that hold
+ *   no token of the batch are left as they are.  Sequences share no pages.
+ *   weights_in, weights_out: device fp32 [pages][kv_heads][page_tokens]; they may be the same array; weights_in NULL counts as zeros.
+ *   workspace: as for vitint_paged_attention, >= vitint_cache_weigh_workspace_bytes() bytes.
+ *   Other arguments, rules and errors as vitint_paged_attention. */
+size_t vitint_cache_weigh_workspace_bytes(const vitint_cache* cache, const vitint_cache_batch* batch);
+int vitint_cache_weigh(const void* q, int32_t q_type, int64_t tokens, int32_t q_heads, int64_t q_token_stride, int64_t q_head_stride,
+                       const float* lse, const vitint_cache* cache, const vitint_cache_batch* batch, float scale, int32_t causal,
+                       int32_t window, const float* weights_in, float* weights_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Eviction by accumulated weight.  Of each sequence and head of the cache the first `sinks` tokens, the last `recent` ones and, of
  *   the others, those of largest weight are kept, `budget` in all (all of a sequence that has no more); equal weights go to the

@@ -137,6 +137,10 @@ def lib():
         L.vitint_paged_attention_workspace_bytes.argtypes = [c_int32, c_char_p, c_char_p]
         L.vitint_paged_attention.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_int64, c_int64, c_char_p, c_char_p, c_float, c_int32,
                                              c_int32, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.vitint_cache_weigh_workspace_bytes.restype = c_size_t
+        L.vitint_cache_weigh_workspace_bytes.argtypes = [c_char_p, c_char_p]
+        L.vitint_cache_weigh.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_int64, c_int64, c_void_p, c_char_p, c_char_p, c_float, c_int32,
+                                         c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.vitint_cache_evict.argtypes = [c_char_p, c_char_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
                                          c_void_p]
         L.vitint_layernorm_quantize.argtypes = [c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_float,
@@ -810,6 +814,32 @@ def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch
     _check(lib().vitint_paged_attention(q.data_ptr(), kind, tokens, heads, qs[0], qs[1], dc, db, scale, int(bool(causal)), window, out.data_ptr(),
                                         os[0], os[1], _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream()), where)
     return out if lse is None else (out, lse)
+
+
+def vitint_cache_weigh_workspace_bytes(cache: PagedCache, batch: CacheBatch) -> int:
+    return int(lib().vitint_cache_weigh_workspace_bytes(cache.desc(), batch.desc()))
+
+
+def vitint_cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: CacheBatch, scale: float,
+                       weights_in: torch.Tensor | None, weights_out: torch.Tensor, causal: bool = True, window: int = 0,
+                       workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Adds the attention weight that every cached token of the batch receives from the queries (with the lse that
+    vitint_paged_attention returned for them) to weights_in [pages, kv_heads, page_tokens] (None: to zero).  Returns weights_out."""
+    where = "vitint_cache_weigh"
+    kind = _queries(q, cache, batch, where)
+    tokens, heads = q.shape[0], q.shape[1]
+    _array(lse, where, "lse", torch.float32, (tokens, heads))
+    for name, t in (("weights_in", weights_in), ("weights_out", weights_out)):
+        if t is not None:
+            _array(t, where, name, torch.float32, tuple(cache.k.shape[:3]))
+    dc, db = cache.desc(where), batch.desc(where)
+    if workspace is None:
+        workspace = torch.empty(lib().vitint_cache_weigh_workspace_bytes(dc, db), dtype=torch.uint8, device=q.device)
+    _here(where, lse, weights_in, weights_out, workspace)
+    qs = q.stride()
+    _check(lib().vitint_cache_weigh(q.data_ptr(), kind, tokens, heads, qs[0], qs[1], lse.data_ptr(), dc, db, scale, int(bool(causal)), window,
+                                    _ptr(weights_in), weights_out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), where)
+    return weights_out
 
 
 def vitint_cache_evict(cache: PagedCache, batch: CacheBatch, weights: torch.Tensor, budget: int, new_table: torch.Tensor, sinks: int = 0,

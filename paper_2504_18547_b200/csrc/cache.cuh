@@ -11,7 +11,7 @@
 
 namespace vitint {
 
-constexpr int64_t CACHE_MAX_LENGTH = 1ll << 30;
+constexpr int64_t CACHE_MAX_LENGTH = 1ll << 29;
 
 inline bool aligned16_elements(int64_t n, int size) { return (n * size) % 16 == 0; }
 inline int dtype_bytes(int type) { return type == VITINT_F32 ? 4 : type == VITINT_I8 ? 1 : 2; }
@@ -153,7 +153,7 @@ __device__ __forceinline__ Sequence sequence_of(const SequenceView& s, int b) {
 
 // Page of a sequence's token; one outside the cache is reported and given as `pages` (nothing lies there: the TMA fills in zeros).
 __device__ __forceinline__ int page_of(const SequenceView& s, int b, int token) {
-    const int p = __ldg(s.page_table + (long long)b * s.table_stride + (token >> s.page_shift));
+    const int p = s.page_table[(long long)b * s.table_stride + (token >> s.page_shift)];
     if ((unsigned)p < (unsigned)s.pages) return p;
     report_bad_data();
     return s.pages;

@@ -2,5 +2,6 @@
 #include "qk_norm_rotate.cu"
 #include "cache_evict.cu"
 #include "paged_attention.cu"
+#include "cache_weigh.cu"
 
 int vitint::take_cache_status_word() { return take_status_word(); }

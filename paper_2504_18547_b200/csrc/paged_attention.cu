@@ -9,7 +9,7 @@
 // The contractions are warp-level m16n8k16 products: sixteen rows are all there are, and a 128-row tcgen05 tile would be empty at
 // seven eighths.  8-bit codes become 16-bit operands in registers (integers up to 128 are exact in both types): the order of the
 // contraction's index is free as long as both sides agree, so a thread takes its codes as they lie, sixteen bytes at a time.
-#include "paged_plan.cuh"
+#include "paged_tiles.cuh"
 
 namespace vitint {
 namespace {
@@ -74,26 +74,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
     uint2 v;
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
-}
-
-// Two signed bytes, one in the low byte of each half of `two` (other bytes anything), as exact 16-bit floats.
-// bf16: the seven low bits lie in the significand of 128 .. 255, and the sign bit turns the 128 that is taken off into 256.
-// f16: all eight bits, offset by 128, lie in the significand of 1024 .. 1279.
-template <typename T>
-__device__ __forceinline__ uint32_t codes_to_16(uint32_t two);
-template <>
-__device__ __forceinline__ uint32_t codes_to_16<__nv_bfloat16>(uint32_t two) {
-    const uint32_t low = (two & 0x007F007Fu) | 0x43004300u, off = (two & 0x00800080u) | 0x43004300u;
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(low), "r"(off));
-    return r;
-}
-template <>
-__device__ __forceinline__ uint32_t codes_to_16<__half>(uint32_t two) {
-    const uint32_t u = ((two & 0x00FF00FFu) ^ 0x00800080u) | 0x64006400u;
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(0x64806480u));        // 1152
-    return r;
 }
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
@@ -174,7 +154,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     grid_dependency_launch();
     if (warp == 0) {
         bool bad = false;
-        const Stretch r = plan_stretch<KT>(P.plan, blockIdx.x, gridDim.x, bad);
+        const Stretch r = plan_stretch<QueryRuns<KT>>(P.plan, blockIdx.x, gridDim.x, bad);
         if (lane == 0) {
             *shared_stretch = r;
             P.notes[blockIdx.x] = join_note(r, blockIdx.x);
@@ -182,7 +162,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
     }
     __syncthreads();
-    StretchWalk<KT> w;
+    StretchWalk<QueryRuns<KT>> w;
     w.begin(P.plan, *shared_stretch);
     bool ok = true;
     int stage = 0;
@@ -198,7 +178,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         int issued = 0;
         for (; ok && w.more(); w.next(P.plan)) {
             for (int t = w.tile; t < w.end; ++t) {
-                const int key = w.first_key + t * KT + lane * P.page_rows;
+                const int key = w.first + t * KT + lane * P.page_rows;
                 const bool mine = lane < copies && key < w.s.length;
                 const int page = mine ? page_of(P.plan.seq, w.b, key) : 0;
                 const bool inside = mine && page < P.plan.seq.pages;
@@ -251,12 +231,12 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 if (CODES) {                                             // channels as the codes lie: 16 (c + 4 (k / 4)) + 4 (k % 4) + 0 .. 3
-                    const uint2 v = live ? __ldg(reinterpret_cast<const uint2*>(from + 16 * (c + 4 * (k >> 2)) + 4 * (k & 3))) : make_uint2(0u, 0u);
+                    const uint2 v = live ? *reinterpret_cast<const uint2*>(from + 16 * (c + 4 * (k >> 2)) + 4 * (k & 3)) : make_uint2(0u, 0u);
                     qa[k][r] = v.x;
                     qa[k][2 + r] = v.y;
                 } else {
-                    qa[k][r] = live ? __ldg(reinterpret_cast<const uint32_t*>(from + 16 * k + 2 * c)) : 0u;
-                    qa[k][2 + r] = live ? __ldg(reinterpret_cast<const uint32_t*>(from + 16 * k + 8 + 2 * c)) : 0u;
+                    qa[k][r] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 2 * c) : 0u;
+                    qa[k][2 + r] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 8 + 2 * c) : 0u;
                 }
             }
             high[r] = !live ? 0 : P.plan.causal ? min(base + i + 1, w.s.length) : w.s.length;
@@ -273,7 +253,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             ok = ok && mbar_wait_warp(bars + 8 * stage, phase, abort_flag);
             if (ok) {
                 const uint32_t kbase = smem + stage * S::STAGE;
-                const int key0 = w.first_key + t * KT + warp * NK;
+                const int key0 = w.first + t * KT + warp * NK;
                 const bool edge = key0 < all_low || key0 + NK > all_high;
                 float s[NT][4];
 #pragma unroll
@@ -549,7 +529,6 @@ paged_rows_join_kernel(const __grid_constant__ RowsParams P) {
 
 inline int rows_grid() { return 2 * sm_count(); }
 inline size_t rows_partial_bytes(int ctas, int head_dim) { return (size_t)ctas * 2 * (16 * head_dim + 32) * 4; }
-inline size_t notes_bytes(int ctas) { return ((size_t)ctas * sizeof(JoinNote) + 255) & ~(size_t)255; }
 
 template <int D, typename T, bool CODES>
 int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cache_batch* batch, void* workspace, cudaStream_t st) {
@@ -578,33 +557,6 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
 }
 
 }  // namespace
-
-// Arguments that the attention and the weighing of the cache share.
-int check_paged_queries(const void* q, int32_t q_type, int64_t tokens, int32_t q_heads, int64_t token_stride, int64_t head_stride,
-                        const vitint_cache* cache, const vitint_cache_batch* batch, float scale, int32_t causal, int32_t window) {
-    if (int rc = check_cache(cache)) return rc;
-    if (int rc = check_batch(cache, batch, true)) return rc;
-    if (!q || tokens <= 0 || q_heads <= 0 || q_heads % cache->kv_heads != 0) return VITINT_ERR_INVALID_ARG;
-    if (q_type != VITINT_BF16 && q_type != VITINT_F16) return VITINT_ERR_INVALID_ARG;
-    if (cache->type != VITINT_I8 && cache->type != q_type) return VITINT_ERR_INVALID_ARG;
-    if (!(scale > 0.0f && scale < INFINITY) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal)) return VITINT_ERR_INVALID_ARG;
-    if (q_heads / cache->kv_heads > 128 || tokens > 0x7fffffffll / 128) return VITINT_ERR_UNSUPPORTED;
-    if (!aligned16(q) || token_stride % 8 != 0 || head_stride % 8 != 0) return VITINT_ERR_ALIGNMENT;
-    if (token_stride <= 0 || head_stride < cache->head_dim) return VITINT_ERR_INVALID_ARG;
-    return VITINT_OK;
-}
-
-inline PlanParams plan_params(const vitint_cache* cache, const vitint_cache_batch* batch, int64_t tokens, int32_t q_heads, int32_t causal,
-                              int32_t window) {
-    PlanParams a{};
-    a.seq = sequence_view(cache, batch, tokens);
-    a.kv_heads = cache->kv_heads;
-    a.group = q_heads / cache->kv_heads;
-    a.causal = causal;
-    a.window = window >= batch->max_length ? 0 : window;
-    return a;
-}
-
 }  // namespace vitint
 
 using namespace vitint;

@@ -1,7 +1,7 @@
 // How the attention kernels over the paged cache share their work out.
 //
-// An item is a head of the cache and a run of a sequence's new tokens (tile_tokens of them, all query heads of the group); its work
-// is a number of key tiles.  All items' key tiles, sequence by sequence, head by head, run by run, form one line, and every CTA
+// An item is, for the attention, a head of the cache and a run of a sequence's new tokens (tile_tokens of them, all query heads of the
+// group); its work is a number of key tiles.  (For the weighing it is a run of keys, and its work the runs of queries.)  All items' tiles, sequence by sequence, head by head, run by run, form one line, and every CTA
 // takes an equal stretch of it: whatever the lengths are, no CTA has more than one tile above the mean.  A stretch that ends inside
 // an item leaves a partial result (row maxima, sums and unnormalised outputs) in the workspace, at most two a CTA, and a second
 // kernel joins them.  The plan is made on the device from the lengths, so a recorded graph may be replayed with others; it is a
@@ -18,29 +18,52 @@ struct PlanParams {
     int causal, window;                   // window 0: none
 };
 
-// Work of run p of a sequence: its first key (a multiple of KT) and its key tiles, at least one (a run that sees no key still
-// writes its rows).
-template <int KT>
-__device__ __forceinline__ int item_tiles(const PlanParams& A, const Sequence& s, int p, int& first_key) {
-    const int i0 = p * A.tile_tokens, i1 = min(s.queries, i0 + A.tile_tokens) - 1, base = s.length - s.queries;
-    const int end = A.causal ? min(base + i1 + 1, s.length) : s.length;
-    first_key = A.window ? max(base + i0 - A.window + 1, 0) / KT * KT : 0;
-    return max((end - first_key + KT - 1) / KT, 1);
-}
-__device__ __forceinline__ int runs_of(const PlanParams& A, const Sequence& s) { return (s.queries + A.tile_tokens - 1) / A.tile_tokens; }
+// What an item is.  runs(): the items of a sequence for one head; tiles(): the steps of work of run p, at least one, and where they
+// begin; uniform(): the steps where every run has the same number, else 0.
 
-// Key tiles of one head of sequence `b` of every lane (0 where b is none).  Whole-warp.
+// Attention: a run of tile_tokens new tokens, a step for every KT keys that they see (a run that sees none still writes its rows).
 template <int KT>
+struct QueryRuns {
+    static __device__ __forceinline__ int runs(const PlanParams& A, const Sequence& s) { return (s.queries + A.tile_tokens - 1) / A.tile_tokens; }
+    static __device__ __forceinline__ int tiles(const PlanParams& A, const Sequence& s, int p, int& first_key) {
+        const int i0 = p * A.tile_tokens, i1 = min(s.queries, i0 + A.tile_tokens) - 1, base = s.length - s.queries;
+        const int end = A.causal ? min(base + i1 + 1, s.length) : s.length;
+        first_key = A.window ? max(base + i0 - A.window + 1, 0) / KT * KT : 0;
+        return max((end - first_key + KT - 1) / KT, 1);
+    }
+    static __device__ __forceinline__ int uniform(const PlanParams& A, const Sequence& s) {
+        int key;
+        return runs(A, s) <= 1 || !A.causal ? tiles(A, s, 0, key) : 0;
+    }
+};
+
+// Weighing: a run of KT keys, a step for every tile_tokens new tokens that see some of them (keys that none sees still get their sum).
+template <int KT>
+struct KeyRuns {
+    static __device__ __forceinline__ int runs(const PlanParams&, const Sequence& s) { return (s.length + KT - 1) / KT; }
+    static __device__ __forceinline__ int tiles(const PlanParams& A, const Sequence& s, int p, int& first_run) {
+        const int base = s.length - s.queries;
+        int from = 0, to = s.queries;
+        if (A.causal) from = max(p * KT - base, 0);
+        if (A.window) to = min(to, p * KT + KT - 1 - base + A.window);
+        first_run = from / A.tile_tokens;
+        return max((to + A.tile_tokens - 1) / A.tile_tokens - first_run, 1);
+    }
+    static __device__ __forceinline__ int uniform(const PlanParams& A, const Sequence& s) {
+        return s.queries <= A.tile_tokens ? 1 : A.causal ? 0 : (s.queries + A.tile_tokens - 1) / A.tile_tokens;
+    }
+};
+
+// Steps of one head of sequence `b` of every lane (0 where b is none).  Whole-warp.
+template <typename Runs>
 __device__ __forceinline__ int sequence_tiles(const PlanParams& A, int b, bool& ok) {
     Sequence s{};
     if (b < A.seq.sequences) s = sequence_of(A.seq, b, ok);
-    const int runs = runs_of(A, s);
-    int sum = 0, key;
-    if (runs <= 4)
-        for (int p = 0; p < runs; ++p) sum += item_tiles<KT>(A, s, p, key);
-    uint32_t many = __ballot_sync(0xffffffffu, runs > 4);
+    const int runs = b < A.seq.sequences ? Runs::runs(A, s) : 0, same = runs ? Runs::uniform(A, s) : 1;
+    int sum = runs * same, first;
+    uint32_t many = __ballot_sync(0xffffffffu, same == 0);
     const int lane = threadIdx.x & 31;
-    while (many) {
+    while (many) {                                                     // the warp's lanes take a sequence's runs
         const int from = __ffs(many) - 1;
         many &= many - 1;
         Sequence t;
@@ -48,7 +71,7 @@ __device__ __forceinline__ int sequence_tiles(const PlanParams& A, int b, bool& 
         t.first = 0;
         t.queries = __shfl_sync(0xffffffffu, s.queries, from);
         int part = 0;
-        for (int p = lane; p < runs_of(A, t); p += 32) part += item_tiles<KT>(A, t, p, key);
+        for (int p = lane; p < Runs::runs(A, t); p += 32) part += Runs::tiles(A, t, p, first);
         part = __reduce_add_sync(0xffffffffu, part);
         if (lane == from) sum = part;
     }
@@ -75,15 +98,15 @@ struct Stretch {
 };
 
 // Whole-warp.  `bad`: whether the host's declarations do not hold.
-template <int KT>
+template <typename Runs>
 __device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, int ctas, bool& bad) {
     const int lane = threadIdx.x & 31;
     bool ok = true;
     int total = 0;                                                     // (the host has checked that all tiles together fit)
-    const int first32 = sequence_tiles<KT>(A, lane, ok);               // kept: most calls have no more sequences
+    const int first32 = sequence_tiles<Runs>(A, lane, ok);               // kept: most calls have no more sequences
     {
         int sum = first32;
-        for (int b0 = 32; b0 < A.seq.sequences; b0 += 32) sum += sequence_tiles<KT>(A, b0 + lane, ok);
+        for (int b0 = 32; b0 < A.seq.sequences; b0 += 32) sum += sequence_tiles<Runs>(A, b0 + lane, ok);
         total = __reduce_add_sync(0xffffffffu, sum) * A.kv_heads;
     }
     bad = __any_sync(0xffffffffu, !ok);
@@ -94,7 +117,7 @@ __device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, in
     r.count = min(per, total - (int)lo);
     int base = 0;                                                      // tiles in front of the block of 32 sequences
     for (int b0 = 0; b0 < A.seq.sequences; b0 += 32) {
-        const int t = b0 ? sequence_tiles<KT>(A, b0 + lane, ok) : first32;
+        const int t = b0 ? sequence_tiles<Runs>(A, b0 + lane, ok) : first32;
         const int all = t * A.kv_heads, sum = warp_inclusive_sum(all);
         const uint32_t hit = __ballot_sync(0xffffffffu, base + sum > (int)lo);
         if (!hit) {
@@ -108,10 +131,15 @@ __device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, in
         r.h = ((int)lo - begin) / tiles;
         begin += r.h * tiles;                                          // ... of its head
         const Sequence s = sequence_of(A.seq, r.b);
-        const int runs = runs_of(A, s);
-        for (int p0 = 0;; p0 += 32) {
-            int key, n = 0;
-            if (p0 + lane < runs) n = item_tiles<KT>(A, s, p0 + lane, key);
+        const int runs = Runs::runs(A, s), same = Runs::uniform(A, s);
+        int p0 = 0;
+        if (same) {
+            p0 = ((int)lo - begin) / same;
+            begin += p0 * same;
+        }
+        for (;; p0 += 32) {
+            int first, n = 0;
+            if (p0 + lane < runs) n = Runs::tiles(A, s, p0 + lane, first);
             const int psum = warp_inclusive_sum(n);
             const uint32_t phit = __ballot_sync(0xffffffffu, begin + psum > (int)lo);
             if (!phit) {
@@ -132,11 +160,11 @@ __device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, in
 }
 
 // The items of a stretch, one after the other.
-template <int KT>
+template <typename Runs>
 struct StretchWalk {
     int b, h, p, left;
     int tile, end;             // this stretch's tiles of the item
-    int tiles, first_key;      // all of the item's tiles
+    int tiles, first;          // all of the item's tiles, and the first key (or run of queries) of them
     Sequence s;
     __device__ __forceinline__ void begin(const PlanParams& A, const Stretch& r) {
         b = r.b; h = r.h; p = r.p; left = r.count; tile = r.tile;
@@ -150,11 +178,11 @@ struct StretchWalk {
         left -= end - tile;
         if (left <= 0) return;
         tile = 0;
-        if (++p == runs_of(A, s)) {
+        if (++p == Runs::runs(A, s)) {
             p = 0;
             if (++h == A.kv_heads) {
                 h = 0;
-                do s = sequence_of(A.seq, ++b); while (s.queries == 0);      // (another item follows: some sequence has it)
+                do s = sequence_of(A.seq, ++b); while (Runs::runs(A, s) == 0);      // (another item follows: some sequence has it)
             }
         }
         load(A);
@@ -163,7 +191,7 @@ struct StretchWalk {
 
 private:
     __device__ __forceinline__ void load(const PlanParams& A) {
-        tiles = item_tiles<KT>(A, s, p, first_key);
+        tiles = Runs::tiles(A, s, p, first);
         end = min(tiles, tile + left);
     }
 };
@@ -186,5 +214,35 @@ __device__ __forceinline__ JoinNote join_note(const Stretch& r, int cta) {
     }
     return n;
 }
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+// Arguments that the attention and the weighing of the cache share.
+inline int check_paged_queries(const void* q, int32_t q_type, int64_t tokens, int32_t q_heads, int64_t token_stride, int64_t head_stride,
+                        const vitint_cache* cache, const vitint_cache_batch* batch, float scale, int32_t causal, int32_t window) {
+    if (int rc = check_cache(cache)) return rc;
+    if (int rc = check_batch(cache, batch, true)) return rc;
+    if (!q || tokens <= 0 || q_heads <= 0 || q_heads % cache->kv_heads != 0) return VITINT_ERR_INVALID_ARG;
+    if (q_type != VITINT_BF16 && q_type != VITINT_F16) return VITINT_ERR_INVALID_ARG;
+    if (cache->type != VITINT_I8 && cache->type != q_type) return VITINT_ERR_INVALID_ARG;
+    if (!(scale > 0.0f && scale < INFINITY) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal)) return VITINT_ERR_INVALID_ARG;
+    if (q_heads / cache->kv_heads > 128 || tokens > 0x7fffffffll / 128) return VITINT_ERR_UNSUPPORTED;
+    if (!aligned16(q) || token_stride % 8 != 0 || head_stride % 8 != 0) return VITINT_ERR_ALIGNMENT;
+    if (token_stride <= 0 || head_stride < cache->head_dim) return VITINT_ERR_INVALID_ARG;
+    return VITINT_OK;
+}
+
+inline PlanParams plan_params(const vitint_cache* cache, const vitint_cache_batch* batch, int64_t tokens, int32_t q_heads, int32_t causal,
+                              int32_t window) {
+    PlanParams a{};
+    a.seq = sequence_view(cache, batch, tokens);
+    a.kv_heads = cache->kv_heads;
+    a.group = q_heads / cache->kv_heads;
+    a.causal = causal;
+    a.window = window >= batch->max_length ? 0 : window;
+    return a;
+}
+
+inline size_t notes_bytes(int ctas) { return ((size_t)ctas * sizeof(JoinNote) + 255) & ~(size_t)255; }
 
 }  // namespace vitint

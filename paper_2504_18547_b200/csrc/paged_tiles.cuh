@@ -1,0 +1,96 @@
+// What the tensor-core kernels over the paged cache share: 16-bit products on tcgen05, query tiles, and 8-bit codes as 16-bit operands.
+#pragma once
+
+#include "paged_plan.cuh"
+
+namespace vitint {
+namespace ptx {
+
+// Instruction descriptor of a 16-bit MMA with fp32 accumulators: accumulator format F32 (1) in bits [4,6), operand format in [7,10) and
+// [10,13) (0 fp16, 1 bf16), B major-ness in bit 16 (1 = N contiguous), N >> 3 in [17,23), M >> 4 in [24,29).
+__host__ __device__ inline uint32_t idesc_f16(int m, int n, bool bf16, int b_mn_major) {
+    uint32_t d = 1u << 4;
+    if (bf16) d |= (1u << 7) | (1u << 10);
+    d |= (uint32_t)b_mn_major << 16;
+    d |= (uint32_t)(n >> 3) << 17;
+    d |= (uint32_t)(m >> 4) << 24;
+    return d;
+}
+// D[tmem] (+)= A[smem] * B[smem], 16-bit operands.  One thread issues.
+__device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+        "}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// The same with A in tensor memory: its row in the lane, two elements in each 32-bit column.
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+}  // namespace ptx
+
+// Two signed bytes, one in the low byte of each half of `two` (other bytes anything), as exact 16-bit floats.
+// bf16: the seven low bits lie in the significand of 128 .. 255, and the sign bit turns the 128 that is taken off into 256.
+// f16: all eight bits, offset by 128, lie in the significand of 1024 .. 1279.
+template <typename T>
+__device__ __forceinline__ uint32_t codes_to_16(uint32_t two);
+template <>
+__device__ __forceinline__ uint32_t codes_to_16<__nv_bfloat16>(uint32_t two) {
+    const uint32_t low = (two & 0x007F007Fu) | 0x43004300u, off = (two & 0x00800080u) | 0x43004300u;
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(low), "r"(off));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t codes_to_16<__half>(uint32_t two) {
+    const uint32_t u = ((two & 0x00FF00FFu) ^ 0x00800080u) | 0x64006400u;
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(0x64806480u));        // 1152
+    return r;
+}
+// Four codes of a word, in order.
+template <typename T>
+__device__ __forceinline__ uint2 codes_to_16x4(uint32_t four) {
+    return make_uint2(codes_to_16<T>(__byte_perm(four, 0u, 0x4140)), codes_to_16<T>(__byte_perm(four, 0u, 0x4342)));
+}
+
+// A tile of 128 rows of D 16-bit channels as the tensor core wants it: lines of 64 channels, row r of line i at i * 16384 + r * 128, its 16-byte
+// chunk c at slot c ^ (r % 8).  A row of raw codes (as the TMA left them: chunks swizzled likewise) becomes a row of it.
+template <int D, typename T>
+__device__ __forceinline__ void expand_code_row(const uint8_t* raw, uint8_t* tile, int r) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+        const int from = D == 128 ? (j ^ (r & 7)) : (j ^ ((r >> 1) & 3));
+        const uint4 w = *reinterpret_cast<const uint4*>(raw + r * D + from * 16);
+        const uint2 a = codes_to_16x4<T>(w.x), b = codes_to_16x4<T>(w.y), c = codes_to_16x4<T>(w.z), d = codes_to_16x4<T>(w.w);
+        uint8_t* const line = tile + (j >> 2) * 16384 + r * 128;
+        const int chunk = 2 * (j & 3), sw = r & 7;
+        *reinterpret_cast<uint4*>(line + ((chunk ^ sw) << 4)) = make_uint4(a.x, a.y, b.x, b.y);
+        *reinterpret_cast<uint4*>(line + (((chunk + 1) ^ sw) << 4)) = make_uint4(c.x, c.y, d.x, d.y);
+    }
+}
+
+// Queries as rows token by token, the group's heads of a token behind one another: (64 channels, heads, tokens, lines of a head), one line a
+// copy.
+inline bool encode_query_map(CUtensorMap* map, const void* q, int type, int dim, int64_t tokens, int heads, int64_t token_stride, int64_t head_stride,
+                             int group, int box_tokens) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)(dim / 64)};
+    const cuuint64_t strides[3] = {(cuuint64_t)(head_stride * 2), (cuuint64_t)(token_stride * 2), 128};
+    const cuuint32_t box[4] = {64, (cuuint32_t)group, (cuuint32_t)box_tokens, 1}, estr[4] = {1, 1, 1, 1};
+    return fn(map, type == VITINT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(q), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace vitint
