@@ -14,7 +14,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 # The library's translation units; each includes the .cu files of its part (see the files).
 UNITS = {"vitint_lib": ["api", "params", "quantize", "layernorm_compare", "softmax", "gemm", "gemm_direct", "attention_fused", "attention_long",
                         "attention", "softmax_table", "encoder", "selftest", "linear_e2m1"],
-         "cache_lib": ["qk_norm_rotate", "cache_evict", "paged_attention", "cache_weigh"]}
+         "cache_lib": ["qk_norm_rotate", "cache_evict", "paged_attention", "paged_attention_tiles", "cache_weigh"]}
 
 
 def sources():

@@ -10,6 +10,7 @@
 // seven eighths.  8-bit codes become 16-bit operands in registers (integers up to 128 are exact in both types): the order of the
 // contraction's index is free as long as both sides agree, so a thread takes its codes as they lie, sixteen bytes at a time.
 #include "paged_tiles.cuh"
+#include "paged_attention_tiles.cu"
 
 namespace vitint {
 namespace {
@@ -556,6 +557,12 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     return cuda_status(cudaGetLastError());
 }
 
+// Whether a head of the cache has at most as many rows as one warp-level product: the kernel of this file, else that of
+// paged_attention_tiles.cu.
+inline bool few_rows(int q_heads, const vitint_cache* cache, const vitint_cache_batch* batch) {
+    return (int64_t)batch->max_queries * (q_heads / cache->kv_heads) <= PA_ROWS;
+}
+
 }  // namespace
 }  // namespace vitint
 
@@ -563,7 +570,8 @@ using namespace vitint;
 
 extern "C" size_t vitint_paged_attention_workspace_bytes(int32_t q_heads, const vitint_cache* cache, const vitint_cache_batch* batch) {
     if (check_cache(cache) != VITINT_OK || check_batch(cache, batch, true) != VITINT_OK || q_heads <= 0 || q_heads % cache->kv_heads != 0) return 0;
-    return notes_bytes(rows_grid()) + rows_partial_bytes(rows_grid(), cache->head_dim);
+    if (few_rows(q_heads, cache, batch)) return notes_bytes(rows_grid()) + rows_partial_bytes(rows_grid(), cache->head_dim);
+    return notes_bytes(sm_count()) + tiles_partial_bytes(sm_count(), cache->head_dim);
 }
 
 extern "C" int vitint_paged_attention(const void* q, int32_t q_type, int64_t tokens, int32_t q_heads, int64_t q_token_stride,
@@ -577,21 +585,39 @@ extern "C" int vitint_paged_attention(const void* q, int32_t q_type, int64_t tok
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
         workspace_bytes < vitint_paged_attention_workspace_bytes(q_heads, cache, batch))
         return VITINT_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool codes = cache->type == VITINT_I8, bf16 = q_type == VITINT_BF16;
+    if (!few_rows(q_heads, cache, batch)) {
+        TilesParams P{};
+        P.plan = plan_params(cache, batch, tokens, q_heads, causal, window);
+        P.half_tokens = 128 / P.plan.group;
+        P.plan.tile_tokens = 2 * P.half_tokens;
+        P.out = out; P.lse = lse;
+        P.k_steps = cache->k_steps; P.v_steps = cache->v_steps;
+        P.out_token = out_token_stride; P.out_head = out_head_stride;
+        P.q_heads = q_heads;
+        P.c = (float)((double)scale * 1.4426950408889634);
+        auto go = [&](auto launch) { return launch(P, q, tokens, q_token_stride, q_head_stride, cache, batch, workspace, st); };
+        if (cache->head_dim == 64) {
+            if (codes) return bf16 ? go(paged_tiles_launch<64, __nv_bfloat16, true>) : go(paged_tiles_launch<64, __half, true>);
+            return bf16 ? go(paged_tiles_launch<64, __nv_bfloat16, false>) : go(paged_tiles_launch<64, __half, false>);
+        }
+        if (codes) return bf16 ? go(paged_tiles_launch<128, __nv_bfloat16, true>) : go(paged_tiles_launch<128, __half, true>);
+        return bf16 ? go(paged_tiles_launch<128, __nv_bfloat16, false>) : go(paged_tiles_launch<128, __half, false>);
+    }
     RowsParams P{};
     P.plan = plan_params(cache, batch, tokens, q_heads, causal, window);
-    if (P.plan.group > PA_ROWS) return VITINT_ERR_UNSUPPORTED;
     P.plan.tile_tokens = PA_ROWS / P.plan.group;
     P.q = q; P.out = out; P.lse = lse;
     P.k_steps = cache->k_steps; P.v_steps = cache->v_steps;
     P.q_token = q_token_stride; P.q_head = q_head_stride; P.out_token = out_token_stride; P.out_head = out_head_stride;
     P.q_heads = q_heads;
     P.c = (float)((double)scale * 1.4426950408889634);
-    cudaStream_t st = (cudaStream_t)stream;
-    const bool codes = cache->type == VITINT_I8, bf16 = q_type == VITINT_BF16;
+    auto go = [&](auto launch) { return launch(P, cache, batch, workspace, st); };
     if (cache->head_dim == 64) {
-        if (codes) return bf16 ? paged_rows_launch<64, __nv_bfloat16, true>(P, cache, batch, workspace, st) : paged_rows_launch<64, __half, true>(P, cache, batch, workspace, st);
-        return bf16 ? paged_rows_launch<64, __nv_bfloat16, false>(P, cache, batch, workspace, st) : paged_rows_launch<64, __half, false>(P, cache, batch, workspace, st);
+        if (codes) return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, true>) : go(paged_rows_launch<64, __half, true>);
+        return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, false>) : go(paged_rows_launch<64, __half, false>);
     }
-    if (codes) return bf16 ? paged_rows_launch<128, __nv_bfloat16, true>(P, cache, batch, workspace, st) : paged_rows_launch<128, __half, true>(P, cache, batch, workspace, st);
-    return bf16 ? paged_rows_launch<128, __nv_bfloat16, false>(P, cache, batch, workspace, st) : paged_rows_launch<128, __half, false>(P, cache, batch, workspace, st);
+    if (codes) return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, true>) : go(paged_rows_launch<128, __half, true>);
+    return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, false>) : go(paged_rows_launch<128, __half, false>);
 }

@@ -92,7 +92,7 @@ def attention64(q, cache, table, lengths, starts, scale, causal, window):
     contraction and the output once is off by at most
       eps/2 |o|                          the output's rounding (eps/2 is half a step of T),
       eps/2 sum p |v|                    the probabilities' rounding (normal ones),
-      2^-25 L max|v|                     fp16 only: probabilities below the normal range (relative to a maximum of 1),
+      2^-25 L max|v|                     fp16 only: probabilities below the normal range (relative to a maximum of 1 or more),
       (2 ds + 2^-19) sum p |v|           ds: error of a score, (d + 4) 2^-24 scale sum |q||k| for d products and their sum, the step and
                                          the scale, and 2^-24 |s| each for the maximum's subtraction; the sum of exponentials has it
                                          too; 2^-19 covers ex2's 2^-22, the sums' and rescalings' roundings.

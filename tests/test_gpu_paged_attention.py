@@ -200,3 +200,62 @@ def test_offsets_beyond_32_bits(new):
     batch = vt.CacheBatch(at[None].to(torch.int32).cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 1000)
     out, lse = vt.vitint_paged_attention(q.cuda(), vt.PagedCache(k, v), batch, 0.09, want_lse=True)
     pu.check_attention(out, lse, pu.attention64(q, small, order, lengths, starts, 0.09, True, 0))
+
+
+# ---- more rows than one warp-level product: the tensor-core kernel ----------------------------------------------------------------
+
+@pytest.mark.parametrize("ctype,qtype", [(BF16, BF16), (F16, F16), (I8, BF16), (I8, F16)])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("places", [16, 32, 64, 128])
+def test_chunks(dim, places, ctype, qtype):
+    run_case(31, dim, places, qtype, ctype, 2, 4, [(1, 1), (100, 17), (128, 128), (129, 64), (300, 65), (400, 1)])
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+@pytest.mark.parametrize("group,new", [(1, 17), (1, 300), (2, 129), (3, 43), (4, 33), (5, 51), (7, 37), (8, 3), (12, 21), (24, 1), (40, 7), (128, 2)])
+def test_chunk_groups(group, new, ctype):
+    run_case(32, 128, 16, BF16, ctype, 2, group, [(new + 150, new), (new, new), (77, 1)])
+
+
+@pytest.mark.parametrize("ctype", [F16, I8])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 17), (True, 64), (True, 128), (True, 129), (True, 500)])
+def test_chunk_masks(causal, window, ctype):
+    run_case(33, 64, 32, F16, ctype, 2, 3, [(900, 200), (64, 1), (130, 99), (150, 150)], causal, window)
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+def test_chunk_rows_without_keys(ctype):
+    run_case(34, 128, 16, BF16, ctype, 2, 2, [(0, 40), (30, 150), (40, 0), (0, 0), (33, 20)])
+    run_case(35, 64, 32, BF16, ctype, 1, 2, [(0, 40)])
+
+
+def test_chunk_items_are_split():
+    run_case(36, 128, 64, BF16, BF16, 1, 4, [(9000, 40), (3, 1), (777, 300)])
+    run_case(37, 64, 16, F16, I8, 2, 2, [(5000, 130)])
+    run_case(38, 128, 32, F16, F16, 1, 8, [(20000, 20)], window=3000)
+
+
+def test_chunk_peaked_rows():
+    """Maxima that keep growing: the outputs follow several times."""
+    run_case(39, 128, 16, BF16, BF16, 1, 4, [(1700, 100)], q_size=60.0)
+    run_case(40, 64, 16, F16, I8, 1, 4, [(1700, 100)], q_size=40.0)
+
+
+@pytest.mark.parametrize("ctype", [BF16, I8])
+def test_chunk_layouts(ctype):
+    run_case(41, 128, 32, BF16, ctype, 4, 2, [(100, 40), (337, 100)], layout="phd")
+
+
+def test_chunk_tiny_value_steps_in_fp16():
+    g = torch.Generator().manual_seed(42)
+    cache = pu.random_cache(g, 70, 1, 16, 128, I8)
+    cache.v_steps.mul_(1e-4)
+    cache.v_steps[3:6].mul_(300.0)
+    table = pu.random_table(g, [1000], 16, 70)
+    q = torch.randn(40, 4, 128, generator=g).to(F16)
+    starts = torch.tensor([0, 40], dtype=torch.int32)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor([1000], dtype=torch.int32).cuda(), starts.cuda(), 40, 1000)
+    out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.08, want_lse=True)
+    want = list(pu.attention64(q, cache, table, [1000], starts, 0.08, True, 0))
+    want[2] += 2.0 ** -25
+    pu.check_attention(out, lse, want)
