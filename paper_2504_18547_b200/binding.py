@@ -655,18 +655,16 @@ def _require(holds: bool, where: str, what: str) -> None:
         raise VitintError(_ERR_INVALID_ARG, f"{where}: {what}")
 
 
-def _here(where: str, *tensors) -> None:
-    """The call is made on the current device's stream: its tensors are there."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise VitintError(_ERR_INVALID_ARG, f"{where}: a tensor is not on the current device")
+# Single-token calls take a few microseconds on the device, so the checks below are written for few Python steps: a tensor's type, size,
+# device, order and address are asked for once each (head norms: 17 -> 9 us of the host a call, attention 18 -> 11).
+_cuda_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _array(t, where: str, name: str, dtype, shape) -> None:
-    """A contiguous tensor of exactly this type and shape."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise VitintError(_ERR_INVALID_ARG, f"{where}: {name} is a contiguous {dtype} tensor {list(shape)}")
+def _array(t, dtype, count: int, device: int, where: str, name: str) -> int:
+    """Address of a contiguous tensor of `count` elements of this type on the call's device."""
+    if t.dtype is not dtype or t.numel() != count or t.get_device() != device or not t.is_contiguous():
+        raise VitintError(_ERR_INVALID_ARG, f"{where}: {name} is a contiguous {dtype} tensor of {count} elements on the current device")
+    return t.data_ptr()
 
 
 @dataclass
@@ -685,20 +683,24 @@ class PagedCache:
         steps = [torch.empty(shape[:3], device=device) if dtype == torch.int8 else None for _ in range(2)]
         return PagedCache(*kv, *steps)
 
-    def desc(self, where: str = "PagedCache") -> bytes:
+    def desc(self, where: str = "PagedCache", device: int | None = None) -> bytes:
+        """The C descriptor; `device`: where the call is made (the current device)."""
         k, v, ks, vs = self.k, self.v, self.k_steps, self.v_steps
-        pages, heads, places, dim = k.shape
-        stride = k.stride()
-        kind = _DTYPES.get(k.dtype, DTYPE_F32)
-        _require(kind != DTYPE_F32 and v.dtype == k.dtype and v.shape == k.shape and v.stride() == stride and stride[3] == 1, where,
-                 "k and v have one type (bf16, fp16, int8), shape and strides, channels last")
+        device = _cuda_device() if device is None else device
+        shape, stride, dtype = k.shape, k.stride(), k.dtype
+        kind = _DTYPES.get(dtype, DTYPE_F32)
+        if (kind == DTYPE_F32 or len(shape) != 4 or v.dtype is not dtype or v.shape != shape or v.stride() != stride or stride[3] != 1
+                or k.get_device() != device or v.get_device() != device):
+            _require(False, where, "k and v have one type (bf16, fp16, int8), shape and strides, channels last, and are on the current device")
+        pages, heads, places, dim = shape
         if kind == DTYPE_I8:
             _require(ks is not None and vs is not None, where, "codes come with steps")
-            _array(ks, where, "k_steps", torch.float32, (pages, heads, places))
-            _array(vs, where, "v_steps", torch.float32, (pages, heads, places))
+            steps = (_array(ks, torch.float32, pages * heads * places, device, where, "k_steps"),
+                     _array(vs, torch.float32, pages * heads * places, device, where, "v_steps"))
         else:
             _require(ks is None and vs is None, where, "16-bit values have no steps")
-        return _PACK_CACHE(k.data_ptr(), v.data_ptr(), _ptr(ks) or 0, _ptr(vs) or 0, pages, stride[0], stride[1], stride[2], heads, places, dim, kind)
+            steps = (0, 0)
+        return _PACK_CACHE(k.data_ptr(), v.data_ptr(), *steps, pages, stride[0], stride[1], stride[2], heads, places, dim, kind)
 
 
 @dataclass
@@ -711,17 +713,24 @@ class CacheBatch:
     max_queries: int
     max_length: int
 
-    def desc(self, where: str = "CacheBatch") -> bytes:
-        table, lengths, starts = self.page_table, self.lengths, self.query_starts
-        n = lengths.shape[0]
-        _require(table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and table.stride(1) == 1, where,
-                 "page_table is an int32 tensor [sequences, entries]")
-        _array(lengths, where, "lengths", torch.int32, (n,))
-        if starts is not None:
-            _array(starts, where, "query_starts", torch.int32, (n + 1,))
-        stride = table.stride(0) if n > 1 else table.shape[1]
-        _require(self.max_length <= table.shape[1] << 30, where, "max_length fits the page table")
-        return _PACK_BATCH(table.data_ptr(), stride, lengths.data_ptr(), _ptr(starts) or 0, n, self.max_queries, self.max_length)
+    def desc(self, where: str = "CacheBatch", device: int | None = None, page_tokens: int = 128) -> bytes:
+        table, starts = self.page_table, self.query_starts
+        device = _cuda_device() if device is None else device
+        n, entries = _table(table, self.lengths.numel(), device, where, "page_table")
+        if not (0 <= self.max_queries < 1 << 31 and 0 < self.max_length <= table.shape[1] * page_tokens):
+            _require(False, where, "max_queries and max_length are counts, and the page table holds max_length tokens")
+        return _PACK_BATCH(table.data_ptr(), entries, _array(self.lengths, torch.int32, n, device, where, "lengths"),
+                           0 if starts is None else _array(starts, torch.int32, n + 1, device, where, "query_starts"), n, self.max_queries, self.max_length)
+
+
+def _table(t, n: int, device: int, where: str, name: str):
+    """(rows, entries from row to row) of a page table; a row's entries lie behind one another."""
+    shape = t.shape
+    if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
+        raise VitintError(_ERR_INVALID_ARG, f"{where}: {name} is an int32 tensor [sequences, entries] on the current device")
+    if n == 1:
+        return 1, shape[1]
+    return n, t.stride(0)
 
 
 def vitint_qk_norm_rotate(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor | None, head_dim: int, norm: str = "rms", eps: float = 1e-6,
@@ -734,61 +743,88 @@ def vitint_qk_norm_rotate(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tens
     [tokens, heads * head_dim] (slices of one projection's output may be given).  Rotates the first 2 * len(frequencies) channels.
     Returns (q_out [tokens, q_heads, head_dim], k_out: given, or made where there is no cache)."""
     where = "vitint_qk_norm_rotate"
-    tokens, in_type = k.shape[0], _DTYPES.get(k.dtype, DTYPE_I8)
-    rows = [t for t in (q, k, v) if t is not None]
-    for t in rows:
-        _require(t.dim() == 2 and t.shape[0] == tokens and t.dtype == k.dtype and t.stride(1) == 1 and t.shape[1] % head_dim == 0, where,
-                 "q, k and v are rows [tokens, heads * head_dim] of one type")
-    _require(in_type != DTYPE_I8 and norm in _NORMS, where, "rows are fp32, bf16 or fp16, the norm is none, rms or layer")
-    _require((v is None) == (cache is None) and (slots is None) == (cache is None) and (v is None or v.shape[1] == k.shape[1]), where,
-             "v and slots come with a cache")
+    device, f32, dtype = _cuda_device(), torch.float32, k.dtype
+    in_type, kind = _DTYPES.get(dtype, DTYPE_I8), _NORMS.get(norm)
+    if in_type == DTYPE_I8 or kind is None:
+        _require(False, where, "rows are fp32, bf16 or fp16, the norm is none, rms or layer")
+    if (v is None) is not (cache is None) or (slots is None) is not (cache is None):
+        _require(False, where, "v and slots come with a cache")
+    tokens, k_width = k.shape
+    hk = k_width // head_dim
+
+    def rows(t, width):
+        """(address, stride) of input rows."""
+        stride = t.stride()
+        if t.dtype is not dtype or t.shape != (tokens, width) or stride[1] != 1 or width % head_dim or t.get_device() != device:
+            _require(False, where, "q, k and v are rows [tokens, heads * head_dim] of one type on the current device")
+        return t.data_ptr(), stride[0] if tokens > 1 else max(stride[0], width)
+
+    def heads(t, n):
+        """(address, stride) of output rows."""
+        stride = t.stride()
+        if t.dtype is not out_dtype or t.shape != (tokens, n, head_dim) or stride[2] != 1 or (n > 1 and stride[1] != head_dim) or t.get_device() != device:
+            _require(False, where, "q_out and k_out are [tokens, heads, head_dim] of one 16-bit type, heads behind one another")
+        return t.data_ptr(), stride[0] if tokens > 1 else max(stride[0], n * head_dim)
+
     if out_dtype is None:
-        out_dtype = next((t.dtype for t in (q_out, k_out) if t is not None), None) or (
-            cache.k.dtype if cache is not None and cache.k.dtype != torch.int8 else k.dtype if k.dtype != torch.float32 else torch.bfloat16)
-    hq, hk = 0 if q is None else q.shape[1] // head_dim, k.shape[1] // head_dim
-    if q is not None and q_out is None:
-        q_out = torch.empty((tokens, hq, head_dim), dtype=out_dtype, device=k.device)
+        out_dtype = (q_out.dtype if q_out is not None else k_out.dtype if k_out is not None else
+                     cache.k.dtype if cache is not None and cache.k.dtype is not torch.int8 else dtype if dtype is not f32 else torch.bfloat16)
+    pk, sk = rows(k, k_width)
+    pv, sv = (0, 0) if v is None else rows(v, k_width)
+    hq = pq = sq = pqo = sqo = pko = sko = 0
+    if q is not None:
+        width = q.shape[1]
+        hq = width // head_dim
+        pq, sq = rows(q, width)
+        if q_out is None:
+            q_out = torch.empty((tokens, hq, head_dim), dtype=out_dtype, device=k.device)
+        pqo, sqo = heads(q_out, hq)
     if cache is None and k_out is None:
         k_out = torch.empty((tokens, hk, head_dim), dtype=out_dtype, device=k.device)
-    for t, heads in ((q_out, hq), (k_out, hk)):
-        if t is not None:
-            _require(t.dtype == out_dtype and tuple(t.shape) == (tokens, heads, head_dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim),
-                     where, "q_out and k_out are [tokens, heads, head_dim] of one 16-bit type, heads behind one another")
-    for name, t in (("q_gain", q_gain), ("k_gain", k_gain), ("q_offset", q_offset), ("k_offset", k_offset)):
-        if t is not None:
-            _array(t, where, name, torch.float32, (head_dim,))
-    if frequencies is not None:
-        _array(frequencies, where, "frequencies", torch.float64, (frequencies.shape[0],))
+    if k_out is not None:
+        pko, sko = heads(k_out, hk)
+    dims = [0 if t is None else _array(t, f32, head_dim, device, where, "a gain or offset") for t in (q_gain, k_gain, q_offset, k_offset)]
+    rotary = pp = pf = 0
+    if frequencies is not None and frequencies.numel():
+        rotary = 2 * frequencies.numel()
+        pf = _array(frequencies, torch.float64, rotary // 2, device, where, "frequencies")
         _require(positions is not None, where, "frequencies come with positions")
-        _array(positions, where, "positions", torch.int32, (tokens,))
-    dc = None
+        pp = _array(positions, torch.int32, tokens, device, where, "positions")
+    dc, ps, pw = None, 0, 0
     if cache is not None:
-        _array(slots, where, "slots", torch.int64, (tokens,))
+        dc = cache.desc(where, device)
+        ps = _array(slots, torch.int64, tokens, device, where, "slots")
         if weights is not None:
-            _array(weights, where, "weights", torch.float32, tuple(cache.k.shape[:3]))
-        dc = cache.desc(where)
-    _here(where, *rows, q_out, k_out, q_gain, k_gain, q_offset, k_offset, positions, frequencies, slots, weights,
-          *(() if cache is None else (cache.k, cache.v, cache.k_steps, cache.v_steps)))
-    rotary = 0 if frequencies is None else 2 * frequencies.shape[0]
-    d = _PACK_ROTATE(_ptr(q) or 0, k.data_ptr(), _ptr(v) or 0, tokens, 0 if q is None else _ld(q), _ld(k), 0 if v is None else _ld(v),
-                     hq, hk, head_dim, in_type, _NORMS[norm], eps, _ptr(q_gain) or 0, _ptr(k_gain) or 0, _ptr(q_offset) or 0, _ptr(k_offset) or 0,
-                     (_ptr(positions) or 0) if rotary else 0, (_ptr(frequencies) or 0) if rotary else 0, rotary, int(bool(pairs)),
-                     _ptr(q_out) or 0, _ptr(k_out) or 0, 0 if q_out is None else max(q_out.stride(0), hq * head_dim if tokens == 1 else 0),
-                     0 if k_out is None else max(k_out.stride(0), hk * head_dim if tokens == 1 else 0), _DTYPES.get(out_dtype, DTYPE_F32), 0,
-                     _ptr(slots) or 0, _ptr(weights) or 0)
-    _check(lib().vitint_qk_norm_rotate(d, dc, _stream()), where)
+            pw = _array(weights, f32, cache.k.numel() // head_dim, device, where, "weights")
+    code = lib().vitint_qk_norm_rotate(
+        _PACK_ROTATE(pq, pk, pv, tokens, sq, sk, sv, hq, hk, head_dim, in_type, kind, eps, *dims, pp, pf, rotary, 1 if pairs else 0, pqo, pko, sqo, sko,
+                     _DTYPES.get(out_dtype, DTYPE_F32), 0, ps, pw), dc, _stream())
+    if code != 0:
+        raise VitintError(code, where)
     return q_out, k_out
 
 
-def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, where: str):
-    _require(q.dim() == 3 and q.shape[2] == cache.k.shape[3] and q.stride(2) == 1, where, "q is [tokens, q_heads, head_dim], channels last")
+def _workspace(t: torch.Tensor, device: int, where: str) -> int:
+    """Bytes of a caller's workspace."""
+    if t.get_device() != device or not t.is_contiguous():
+        _require(False, where, "workspace is a contiguous tensor on the current device")
+    return t.nbytes
+
+
+def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, where: str, device: int):
+    """(tokens, heads, type, strides, descriptors) of a call's queries, cache and batch."""
+    shape, stride, kv = q.shape, q.stride(), cache.k.shape
+    if len(shape) != 3 or shape[2] != kv[-1] or stride[2] != 1 or q.get_device() != device:
+        _require(False, where, "q is [tokens, q_heads, head_dim], channels last, on the current device")
     _require(batch.query_starts is not None, where, "the batch names the queries' rows")
-    _here(where, q, cache.k, cache.v, cache.k_steps, cache.v_steps, batch.page_table, batch.lengths, batch.query_starts)
-    return _DTYPES.get(q.dtype, DTYPE_F32)
+    # a single token's or head's stride is nothing that is stepped by
+    head = stride[1] if shape[1] > 1 else max(stride[1], shape[2])
+    return (shape[0], shape[1], _DTYPES.get(q.dtype, DTYPE_F32), stride[0] if shape[0] > 1 else shape[1] * head, head, cache.desc(where, device),
+            batch.desc(where, device, kv[2]))
 
 
 def vitint_paged_attention_workspace_bytes(q_heads: int, cache: PagedCache, batch: CacheBatch) -> int:
-    return int(lib().vitint_paged_attention_workspace_bytes(q_heads, cache.desc(), batch.desc()))
+    return int(lib().vitint_paged_attention_workspace_bytes(q_heads, cache.desc(), batch.desc(page_tokens=cache.k.shape[2])))
 
 
 def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, scale: float, causal: bool = True, window: int = 0,
@@ -797,27 +833,36 @@ def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch
     """Attention of every sequence's new tokens (rows of q [tokens, q_heads, head_dim]) over what the cache holds of it.  Returns
     out, or (out, lse [tokens, q_heads]) where lse is given or wanted."""
     where = "vitint_paged_attention"
-    kind = _queries(q, cache, batch, where)
-    tokens, heads = q.shape[0], q.shape[1]
+    device = _cuda_device()
+    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, where, device)
+    L = lib()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _require(out.shape == q.shape and out.dtype == q.dtype and out.stride(2) == 1, where, "out has the shape and type of q, channels last")
-    if lse is None and want_lse:
-        lse = torch.empty((tokens, heads), device=q.device)
+        out = torch.empty_like(q)
+    elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.get_device() != device:
+        _require(False, where, "out has the shape and type of q, channels last, and is on the current device")
+    stride = out.stride()
+    out_head = stride[1] if heads > 1 else max(stride[1], out.shape[2])
     if lse is not None:
-        _array(lse, where, "lse", torch.float32, (tokens, heads))
-    dc, db = cache.desc(where), batch.desc(where)
+        lse_at = _array(lse, torch.float32, tokens * heads, device, where, "lse")
+    elif want_lse:
+        lse = q.new_empty((tokens, heads), dtype=torch.float32)
+        lse_at = lse.data_ptr()
+    else:
+        lse_at = None
     if workspace is None:
-        workspace = torch.empty(lib().vitint_paged_attention_workspace_bytes(heads, dc, db), dtype=torch.uint8, device=q.device)
-    _here(where, out, lse, workspace)
-    qs, os = q.stride(), out.stride()
-    _check(lib().vitint_paged_attention(q.data_ptr(), kind, tokens, heads, qs[0], qs[1], dc, db, scale, int(bool(causal)), window, out.data_ptr(),
-                                        os[0], os[1], _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream()), where)
+        size = L.vitint_paged_attention_workspace_bytes(heads, dc, db)
+        workspace = q.new_empty(size, dtype=torch.uint8)
+    else:
+        size = _workspace(workspace, device, where)
+    code = L.vitint_paged_attention(q.data_ptr(), kind, tokens, heads, q_token, q_head, dc, db, scale, 1 if causal else 0, window, out.data_ptr(),
+                                    stride[0] if tokens > 1 else heads * out_head, out_head, lse_at, workspace.data_ptr(), size, _stream())
+    if code != 0:
+        raise VitintError(code, where)
     return out if lse is None else (out, lse)
 
 
 def vitint_cache_weigh_workspace_bytes(cache: PagedCache, batch: CacheBatch) -> int:
-    return int(lib().vitint_cache_weigh_workspace_bytes(cache.desc(), batch.desc()))
+    return int(lib().vitint_cache_weigh_workspace_bytes(cache.desc(), batch.desc(page_tokens=cache.k.shape[2])))
 
 
 def vitint_cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, batch: CacheBatch, scale: float,
@@ -826,19 +871,20 @@ def vitint_cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, ba
     """Adds the attention weight that every cached token of the batch receives from the queries (with the lse that
     vitint_paged_attention returned for them) to weights_in [pages, kv_heads, page_tokens] (None: to zero).  Returns weights_out."""
     where = "vitint_cache_weigh"
-    kind = _queries(q, cache, batch, where)
-    tokens, heads = q.shape[0], q.shape[1]
-    _array(lse, where, "lse", torch.float32, (tokens, heads))
-    for name, t in (("weights_in", weights_in), ("weights_out", weights_out)):
-        if t is not None:
-            _array(t, where, name, torch.float32, tuple(cache.k.shape[:3]))
-    dc, db = cache.desc(where), batch.desc(where)
+    device, f32 = _cuda_device(), torch.float32
+    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, where, device)
+    L = lib()
+    places = cache.k.numel() // q.shape[2]
     if workspace is None:
-        workspace = torch.empty(lib().vitint_cache_weigh_workspace_bytes(dc, db), dtype=torch.uint8, device=q.device)
-    _here(where, lse, weights_in, weights_out, workspace)
-    qs = q.stride()
-    _check(lib().vitint_cache_weigh(q.data_ptr(), kind, tokens, heads, qs[0], qs[1], lse.data_ptr(), dc, db, scale, int(bool(causal)), window,
-                                    _ptr(weights_in), weights_out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()), where)
+        size = L.vitint_cache_weigh_workspace_bytes(dc, db)
+        workspace = q.new_empty(size, dtype=torch.uint8)
+    else:
+        size = _workspace(workspace, device, where)
+    code = L.vitint_cache_weigh(q.data_ptr(), kind, tokens, heads, q_token, q_head, _array(lse, f32, tokens * heads, device, where, "lse"), dc, db, scale,
+                                1 if causal else 0, window, None if weights_in is None else _array(weights_in, f32, places, device, where, "weights_in"),
+                                _array(weights_out, f32, places, device, where, "weights_out"), workspace.data_ptr(), size, _stream())
+    if code != 0:
+        raise VitintError(code, where)
     return weights_out
 
 
@@ -847,18 +893,19 @@ def vitint_cache_evict(cache: PagedCache, batch: CacheBatch, weights: torch.Tens
     """Keeps `budget` tokens of every sequence and head (the first `sinks`, the last `recent`, of the others those of largest weight)
     and copies them to the pages of new_table.  Returns (kept [sequences, kv_heads, budget], counts [sequences])."""
     where = "vitint_cache_evict"
-    n, heads = batch.lengths.shape[0], cache.k.shape[1]
-    _require(budget > 0, where, "a budget of at least one token")
-    _array(weights, where, "weights", torch.float32, tuple(cache.k.shape[:3]))
-    _require(new_table.dtype == torch.int32 and new_table.dim() == 2 and new_table.shape[0] == n and new_table.stride(1) == 1, where,
-             "new_table is an int32 tensor [sequences, entries]")
+    device, i32 = _cuda_device(), torch.int32
+    n, (_, heads, places, dim) = batch.lengths.numel(), cache.k.shape
+    _require(0 < budget < 1 << 31, where, "a budget of at least one token")
     if kept is None:
-        kept = torch.empty((n, heads, budget), dtype=torch.int32, device=weights.device)
+        kept = weights.new_empty((n, heads, budget), dtype=i32)
     if counts is None:
-        counts = torch.empty(n, dtype=torch.int32, device=weights.device)
-    _array(kept, where, "kept", torch.int32, (n, heads, budget))
-    _array(counts, where, "counts", torch.int32, (n,))
-    _here(where, cache.k, cache.v, cache.k_steps, cache.v_steps, batch.page_table, batch.lengths, weights, new_table, kept, counts)
-    _check(lib().vitint_cache_evict(cache.desc(where), batch.desc(where), weights.data_ptr(), budget, sinks, recent, new_table.data_ptr(),
-                                    new_table.stride(0) if n > 1 else new_table.shape[1], kept.data_ptr(), counts.data_ptr(), _stream()), where)
+        counts = weights.new_empty(n, dtype=i32)
+    _, entries = _table(new_table, n, device, where, "new_table")
+    _require(budget <= new_table.shape[1] * places, where, "the rows of new_table hold the budget")
+    code = lib().vitint_cache_evict(cache.desc(where, device), batch.desc(where, device, places),
+                                    _array(weights, torch.float32, cache.k.numel() // dim, device, where, "weights"), budget, sinks, recent,
+                                    new_table.data_ptr(), entries, _array(kept, i32, n * heads * budget, device, where, "kept"),
+                                    _array(counts, i32, n, device, where, "counts"), _stream())
+    if code != 0:
+        raise VitintError(code, where)
     return kept, counts
