@@ -1,10 +1,13 @@
 // Eviction from the paged cache by accumulated attention weight: which tokens stay, and their move to other pages.
 //
-// Selection, one block for a sequence and head: the `need`-th largest weight among the tokens that are neither sinks nor recent, by a radix
-// search over the weights' order-preserving integers (11, 11 and 10 bits: a histogram in shared memory, then the digit in which the
-// count is reached), and then one pass in token order that writes the indices above it and the first ones equal to it.  A thread has a
-// run of consecutive tokens, so that one scan over the threads gives every kept token its rank.
-// Move: bound by HBM, sixteen bytes a thread and access, rows of keys and values side by side.
+// Selection, one to eight blocks (a cluster) for a sequence and head: the `need`-th largest weight among the tokens that are neither sinks nor
+// recent, by a radix search over the weights' order-preserving integers (11, 11 and 10 bits: a histogram in every block's shared memory,
+// summed over the cluster, then the digit in which the count is reached), and then one pass in token order that writes the indices above
+// it and the first ones equal to it.  The weights are read once and stay in shared memory.  Bound by latency: three histograms and their sums
+// follow one another; clusters are as large as the GPU has room for and a block has 2048 tokens left.
+// 65,536 tokens x 8 heads: 120 -> EVICT_LONG us against one block a head that reads its weights anew for every pass.
+// Move: bound by HBM.  A warp takes 32 kept tokens: its lanes look up where they lie and go, then all of them copy row after row, sixteen bytes a
+// lane, eight rows under way.
 #include "cache.cuh"
 
 namespace vitint {
@@ -12,6 +15,7 @@ namespace {
 
 constexpr int EV_THREADS = 1024;
 constexpr int EV_BINS = 2048;
+constexpr int EV_HELD = 40960;                                        // weights that a block keeps
 
 struct EvictParams {
     SequenceView seq;
@@ -53,12 +57,31 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
     return base + s - v;
 }
 
+// ---- clusters of blocks --------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t v; asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(v)); return v; }
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t v; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(v)); return v; }
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t remote_word(const uint32_t* mine, uint32_t rank) {         // the same variable of another block
+    uint32_t addr = ptx::smem_addr(mine), at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at));                     // (ordered by the barriers around)
+    return v;
+}
+
+// Block `rank` of a cluster takes the rank-th part of a sequence's tokens.  held: tokens whose weights fit the dynamic shared memory; a part
+// that is longer is read from memory in every pass.
 __global__ void __launch_bounds__(EV_THREADS)
-evict_select_kernel(const __grid_constant__ EvictParams P) {
-    __shared__ uint32_t bins[EV_BINS];
+evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
+    extern __shared__ uint32_t ev_keys[];
+    __shared__ uint32_t bins[2][EV_BINS];
     __shared__ unsigned long long warp_sums[32];
     __shared__ uint32_t found[2];                                      // the digit, and how many are still wanted inside it
-    const int h = blockIdx.x, b = blockIdx.y, t = threadIdx.x;
+    __shared__ uint32_t larger_of[33], equal_of[33];                   // counts of the block's warps, then of the block
+    const int blocks = (int)cluster_size(), rank = (int)cluster_rank();
+    const int h = blockIdx.x / blocks, b = blockIdx.y, t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    for (int i = t; i < EV_BINS; i += EV_THREADS) bins[0][i] = 0u;
     grid_dependency_wait();
     grid_dependency_launch();
     bool ok = true;
@@ -66,63 +89,112 @@ evict_select_kernel(const __grid_constant__ EvictParams P) {
     if (!ok && t == 0) report_bad_data();
     const int count = min(length, P.budget);
     int* const kept = P.kept + ((long long)b * P.kv_heads + h) * P.budget;
-    if (h == 0 && t == 0) P.counts[b] = count;
-    for (int i = count + t; i < P.budget; i += EV_THREADS) kept[i] = -1;
-    if (length <= P.budget) {
-        for (int i = t; i < length; i += EV_THREADS) kept[i] = i;
+    const int t0 = rank * EV_THREADS + t, all = blocks * EV_THREADS;
+    if (h == 0 && t0 == 0) P.counts[b] = count;
+    for (int i = count + t0; i < P.budget; i += all) kept[i] = -1;
+    const int first = P.sinks, last = length - P.recent, need = P.budget - P.sinks - P.recent;
+    if (length <= P.budget) {                                          // (the same for all blocks of the cluster)
+        for (int i = t0; i < length; i += all) kept[i] = i;
         return;
     }
-    const int first = P.sinks, last = length - P.recent, need = P.budget - P.sinks - P.recent;
-    for (int i = t; i < P.sinks; i += EV_THREADS) kept[i] = i;
-    for (int i = t; i < P.recent; i += EV_THREADS) kept[P.budget - P.recent + i] = last + i;
+    for (int i = t0; i < P.sinks; i += all) kept[i] = i;
+    for (int i = t0; i < P.recent; i += all) kept[P.budget - P.recent + i] = last + i;
     if (need == 0) return;
+
+    const int part = (last - first + blocks - 1) / blocks, begin = min(first + rank * part, last), n = min(part, last - begin);
     const int shift = P.seq.page_shift, mask = (1 << shift) - 1;
-    auto key_of = [&](int i) {
-        const int p = page_of(P.seq, b, i);
-        return weight_key(p < P.seq.pages ? P.weights[(((long long)p * P.kv_heads + h) << shift) + (i & mask)] : 0.0f);
+    auto read_key = [&](int i) {
+        const int p = page_of(P.seq, b, begin + i);
+        return weight_key(p < P.seq.pages ? P.weights[(((long long)p * P.kv_heads + h) << shift) + ((begin + i) & mask)] : 0.0f);
     };
+    const bool in_shared = n <= held;
+    auto key_of = [&](int i) { return in_shared ? ev_keys[i] : read_key(i); };
+    if (in_shared) {
+#pragma unroll 8
+        for (int i = t; i < n; i += EV_THREADS) ev_keys[i] = read_key(i);
+    }
+    __syncthreads();
     uint32_t prefix = 0, known = 0;                                    // digits found so far, and their bits
     uint32_t want = (uint32_t)need;
+#pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-        for (int i = t; i < EV_BINS; i += EV_THREADS) bins[i] = 0u;
-        __syncthreads();
-        for (int i = first + t; i < last; i += EV_THREADS) {
+        const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t digits = pass == 2 ? 1023u : 2047u;
+        uint32_t* const mine = bins[pass & 1];
+        for (int i = t; i < n; i += EV_THREADS) {
             const uint32_t k = key_of(i);
-            if ((k & known) == prefix) atomicAdd(&bins[(k >> low) & ((1u << width) - 1u)], 1u);
+            // equal digits of a warp are counted together: many tokens have the same weight (none), and their additions would queue up
+            if ((k & known) == prefix) {
+                const uint32_t digit = (k >> low) & digits, same = __match_any_sync(__activemask(), digit);
+                if (lane == __ffs(same) - 1) atomicAdd(&mine[digit], (uint32_t)__popc(same));
+            }
         }
-        __syncthreads();
-        // bins from the largest digit down: thread t has digits EV_BINS-1-2t and EV_BINS-2-2t
+        cluster_barrier();
+        // (the other histogram was last read in front of this barrier)
+        for (int i = t; i < EV_BINS; i += EV_THREADS) bins[(pass + 1) & 1][i] = 0u;
+        // digits from the largest down: thread t has EV_BINS-1-2t and EV_BINS-2-2t, over all blocks
         const uint32_t d0 = EV_BINS - 1 - 2 * t, d1 = d0 - 1;
-        const uint32_t n0 = bins[d0], n1 = bins[d1];
+        uint32_t n0 = mine[d0], n1 = mine[d1];
+        if (blocks > 1) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r)                                 // (all of them under way at once)
+                if (r < blocks && r != rank) {
+                    n0 += remote_word(&mine[d0], r);
+                    n1 += remote_word(&mine[d1], r);
+                }
+        }
         unsigned long long total;
         const uint32_t above = (uint32_t)block_scan(n0 + n1, warp_sums, total);
         if (above < want && want <= above + n0) { found[0] = d0; found[1] = want - above; }
         else if (above + n0 < want && want <= above + n0 + n1) { found[0] = d1; found[1] = want - above - n0; }
         __syncthreads();
         prefix |= found[0] << low;
-        known |= ((1u << width) - 1u) << low;
+        known |= digits << low;
         want = found[1];
         __syncthreads();
     }
-    // `prefix` is the last weight to stay, `want` of the tokens that have it do
-    const int run = (last - first + EV_THREADS - 1) / EV_THREADS;
-    const int begin = min(first + t * run, last), end = min(begin + run, last);
+    // `prefix` is the last weight to stay, `want` of the tokens that have it do.  A warp has a run of the block's tokens, 32 at a time.
+    const int run = ((n + 1023) / 1024) * 32, from = min(warp * run, n), to = min(from + run, n);
     uint32_t larger = 0, equal = 0;
-    for (int i = begin; i < end; ++i) {
+    for (int i = from + lane; i < to; i += 32) {
         const uint32_t k = key_of(i);
         larger += k > prefix;
         equal += k == prefix;
     }
-    unsigned long long total;
-    const unsigned long long before = block_scan(((unsigned long long)larger << 32) | equal, warp_sums, total);
-    uint32_t ahead = (uint32_t)before;                                 // equal ones in front
-    int* to = kept + P.sinks + (uint32_t)(before >> 32) + min(ahead, want);
-    for (int i = begin; i < end; ++i) {
-        const uint32_t k = key_of(i);
-        if (k > prefix || (k == prefix && ahead < want)) *to++ = i;
-        ahead += k == prefix;
+    larger = __reduce_add_sync(0xffffffffu, larger);
+    equal = __reduce_add_sync(0xffffffffu, equal);
+    if (lane == 0) { larger_of[warp] = larger; equal_of[warp] = equal; }
+    __syncthreads();
+    if (warp == 0) {
+        const uint32_t a = larger_of[lane], e = equal_of[lane];
+        const uint32_t sa = (uint32_t)__reduce_add_sync(0xffffffffu, a), se = (uint32_t)__reduce_add_sync(0xffffffffu, e);
+        uint32_t pa = a, pe = e;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, pa, o), y = __shfl_up_sync(0xffffffffu, pe, o);
+            if (lane >= o) { pa += x; pe += y; }
+        }
+        larger_of[lane] = pa - a;
+        equal_of[lane] = pe - e;
+        if (lane == 0) { larger_of[32] = sa; equal_of[32] = se; }
     }
+    cluster_barrier();
+    uint32_t ahead_larger = larger_of[warp], ahead_equal = equal_of[warp];
+    for (int r = 0; r < rank; ++r) {
+        ahead_larger += remote_word(&larger_of[32], r);
+        ahead_equal += remote_word(&equal_of[32], r);
+    }
+    for (int i0 = from; i0 < to; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t k = i < to ? key_of(i) : 0u;
+        const bool is_larger = i < to && k > prefix, is_equal = i < to && k == prefix;
+        const uint32_t a = __ballot_sync(0xffffffffu, is_larger), e = __ballot_sync(0xffffffffu, is_equal), below = (1u << lane) - 1u;
+        const uint32_t my_equal = ahead_equal + __popc(e & below);
+        if (is_larger || (is_equal && my_equal < want)) kept[P.sinks + ahead_larger + __popc(a & below) + min(my_equal, want)] = begin + i;
+        ahead_larger += __popc(a);
+        ahead_equal += __popc(e);
+    }
+    cluster_barrier();                                                 // the others have read this block's counts
 }
 
 struct MoveParams {
@@ -133,38 +205,88 @@ struct MoveParams {
     uint8_t *k, *v;
     float *k_steps, *v_steps, *weights;
     long long page_bytes, head_bytes, token_bytes;
-    int kv_heads, budget, units;                                       // units: 16-byte pieces of a key row
+    int kv_heads, budget;
 };
 
-// A thread moves one piece of a key or value row; the threads of a row's first piece take its step, and the weight.
+// UNITS: 16-byte pieces of a key row.  Block y: a sequence and head; a warp takes 32 of its kept tokens.
+template <int UNITS>
 __global__ void __launch_bounds__(256)
 evict_move_kernel(const __grid_constant__ MoveParams P) {
+    constexpr int ROWS = 32 / (2 * UNITS) > 0 ? 32 / (2 * UNITS) : 1;   // rows that a warp copies at once
+    constexpr int DEEP = 8;                                            // ... and how often before it stores them
     grid_dependency_wait();
     grid_dependency_launch();
-    const long long index = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int per = 2 * P.units, shift = P.seq.page_shift, mask = (1 << shift) - 1;
-    const long long row = index / per;
-    if (row >= (long long)P.seq.sequences * P.kv_heads * P.budget) return;
-    const int piece = (int)(index - row * per);
-    const int from = P.kept[row];
-    if (from < 0) return;
-    const int to = (int)(row % P.budget), bh = (int)(row / P.budget), b = bh / P.kv_heads, h = bh - b * P.kv_heads;
-    const int old_page = page_of(P.seq, b, from), new_page = P.new_table[b * P.new_stride + (to >> shift)];
-    if ((unsigned)new_page >= (unsigned)P.seq.pages) { report_bad_data(); return; }
-    if (old_page >= P.seq.pages) return;
-    const bool is_v = piece >= P.units;
-    const int unit = piece - (is_v ? P.units : 0);
-    uint8_t* const base = is_v ? P.v : P.k;
-    const long long inside = h * P.head_bytes + unit * 16;
-    const uint4 w = *reinterpret_cast<const uint4*>(base + old_page * P.page_bytes + (from & mask) * P.token_bytes + inside);
-    *reinterpret_cast<uint4*>(base + new_page * P.page_bytes + (to & mask) * P.token_bytes + inside) = w;
-    if (unit == 0) {
-        const long long a = (((long long)old_page * P.kv_heads + h) << shift) + (from & mask);
-        const long long z = (((long long)new_page * P.kv_heads + h) << shift) + (to & mask);
-        float* const steps = is_v ? P.v_steps : P.k_steps;
-        if (steps) steps[z] = steps[a];
-        if (!is_v) P.weights[z] = P.weights[a];
+    const int lane = threadIdx.x & 31, b = blockIdx.y / P.kv_heads, h = blockIdx.y - b * P.kv_heads, shift = P.seq.page_shift, mask = (1 << shift) - 1;
+    const int to0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * 32, to = to0 + lane;
+    // the lane's token: where its row lies and goes (-1: nowhere)
+    const int from = to < P.budget ? P.kept[(long long)blockIdx.y * P.budget + to] : -1;
+    long long src = -1, dst = -1, z = 0;
+    float weight = 0.0f, k_step = 0.0f, v_step = 0.0f;
+    if (from >= 0) {
+        const int old_page = page_of(P.seq, b, from), new_page = P.new_table[b * P.new_stride + (to >> shift)];
+        if ((unsigned)new_page >= (unsigned)P.seq.pages) {
+            report_bad_data();
+        } else if (old_page < P.seq.pages) {
+            src = old_page * P.page_bytes + (from & mask) * P.token_bytes + h * P.head_bytes;
+            dst = new_page * P.page_bytes + (to & mask) * P.token_bytes + h * P.head_bytes;
+            const long long a = (((long long)old_page * P.kv_heads + h) << shift) + (from & mask);
+            z = (((long long)new_page * P.kv_heads + h) << shift) + (to & mask);
+            weight = P.weights[a];
+            if (P.k_steps) {
+                k_step = P.k_steps[a];
+                v_step = P.v_steps[a];
+            }
+        }
     }
+    const int piece = lane % (2 * UNITS), row0 = lane / (2 * UNITS);
+    uint8_t* const base = piece < UNITS ? P.k : P.v;
+    const int inside = (piece % UNITS) * 16;
+#pragma unroll 1
+    for (int r = 0; r < 32; r += ROWS * DEEP) {
+        uint4 w[DEEP];
+        long long at[DEEP];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            const int row = r + k * ROWS + row0;
+            const long long s = __shfl_sync(0xffffffffu, src, row & 31);
+            at[k] = __shfl_sync(0xffffffffu, dst, row & 31);
+            if (s >= 0) w[k] = *reinterpret_cast<const uint4*>(base + s + inside);
+        }
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k)
+            if (at[k] >= 0) *reinterpret_cast<uint4*>(base + at[k] + inside) = w[k];
+    }
+    if (dst >= 0) {
+        P.weights[z] = weight;
+        if (P.k_steps) {
+            P.k_steps[z] = k_step;
+            P.v_steps[z] = v_step;
+        }
+    }
+}
+
+// Blocks of a cluster: as many as the GPU has room for side by side, while a block has 2048 tokens left.
+inline int evict_cluster(int64_t items, int64_t max_length) {
+    int c = 1;
+    while (c < 8 && items * (2 * c) <= sm_count() && max_length >= 4096 * c) c *= 2;
+    return c;
+}
+
+inline cudaError_t launch_select(const EvictParams& E, int sequences, int cluster, int held, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(E.kv_heads * cluster), (unsigned)sequences);
+    cfg.blockDim = dim3(EV_THREADS);
+    cfg.dynamicSmemBytes = (size_t)held * 4;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, evict_select_kernel, E, held);
 }
 
 }  // namespace
@@ -193,12 +315,26 @@ extern "C" int vitint_cache_evict(const vitint_cache* cache, const vitint_cache_
     M.k = (uint8_t*)cache->k; M.v = (uint8_t*)cache->v; M.k_steps = cache->k_steps; M.v_steps = cache->v_steps; M.weights = weights;
     const int size = dtype_bytes(cache->type);
     M.page_bytes = cache->page_stride * size; M.head_bytes = cache->head_stride * size; M.token_bytes = cache->token_stride * size;
-    M.kv_heads = cache->kv_heads; M.budget = budget; M.units = cache->head_dim * size / 16;
-    const long long rows = (long long)batch->sequences * cache->kv_heads * budget, blocks = (rows * 2 * M.units + 255) / 256;
-    if (blocks > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
+    M.kv_heads = cache->kv_heads; M.budget = budget;
+    const long long items = (long long)batch->sequences * cache->kv_heads;
+    if (items > 65535 || (long long)cache->kv_heads * 8 > 65535) return VITINT_ERR_UNSUPPORTED;      // (blocks along a grid's second dimension)
+    const int cluster = evict_cluster(items, batch->max_length);
+    const int64_t part = (batch->max_length + cluster - 1) / cluster;
+    const int held = part <= EV_HELD ? (int)part : EV_HELD;
+    const int dev = current_device();
+    if (dev < 0) return VITINT_ERR_CUDA;
+    static bool attr_set_dev[MAX_DEVICES] = {};
+    if (!attr_set_dev[dev]) {
+        if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_HELD * 4) != cudaSuccess) return VITINT_ERR_CUDA;
+        attr_set_dev[dev] = true;
+    }
     cudaStream_t st = (cudaStream_t)stream;
-    launch_kernel(evict_select_kernel, dim3(cache->kv_heads, batch->sequences), dim3(EV_THREADS), 0, st, E);
-    if (int rc = cuda_status(cudaGetLastError())) return rc;
-    launch_kernel(evict_move_kernel, dim3((unsigned)blocks), dim3(256), 0, st, M);
+    if (int rc = cuda_status(launch_select(E, batch->sequences, cluster, held, st))) return rc;
+    const dim3 grid((unsigned)((budget + 255) / 256), (unsigned)items);
+    switch (cache->head_dim * size / 16) {
+        case 4: launch_kernel(evict_move_kernel<4>, grid, dim3(256), 0, st, M); break;
+        case 8: launch_kernel(evict_move_kernel<8>, grid, dim3(256), 0, st, M); break;
+        default: launch_kernel(evict_move_kernel<16>, grid, dim3(256), 0, st, M); break;
+    }
     return cuda_status(cudaGetLastError());
 }

@@ -3,12 +3,16 @@
 //   s_rj = scale * step_j (q_r . k_j);  p = 2^(s log2 e - m);  o_r = sum_j (p_rj vstep_j) v_j / sum_j p_rj
 //
 // Bound by HBM: every key and value is read once for a handful of multiplications.  What the kernel has to do is to keep enough
-// bytes in flight on every SM and share the keys out evenly (paged_plan.cuh).  A producer warp copies key tiles (their pages'
-// pieces, one TMA copy a page for keys and one for values) into a ring of about 96 KB a CTA, two CTAs an SM; four warps take a
-// quarter of each tile's keys, each with a running maximum, sum and output of its own, so that they meet only at an item's end.
-// The contractions are warp-level m16n8k16 products: sixteen rows are all there are, and a 128-row tcgen05 tile would be empty at
-// seven eighths.  8-bit codes become 16-bit operands in registers (integers up to 128 are exact in both types): the order of the
-// contraction's index is free as long as both sides agree, so a thread takes its codes as they lie, sixteen bytes at a time.
+// bytes in flight on every SM, few instructions behind them, and share the keys out evenly (paged_plan.cuh).  A producer warp copies key
+// tiles (their pages' pieces, one TMA copy a page for keys and one for values) into a ring; four warps take a quarter of each tile's keys,
+// each with a running maximum, sum and output of its own, so that they meet only at an item's end.
+// The contractions are warp-level m16n8k16 products with the keys (then the channels of the values) as the sixteen rows and the queries
+// as eight columns: S^T = K Q^T, O^T = V^T P^T.  A 128-row tcgen05 tile of queries would be empty at fifteen sixteenths, and queries as the
+// sixteen rows would spend twice the products and registers on the up to eight there mostly are; up to sixteen take two products.
+// 8-bit codes become fp16 operands in registers (exact): the order of the contraction's index is free as long as both sides agree, so a thread
+// takes its codes as they lie, sixteen bytes at a time.
+// Up to eight rows a probability is multiplied as the sum of two 16-bit numbers (the tensor core is idle otherwise), so that only the output is
+// rounded.
 #include "paged_tiles.cuh"
 #include "paged_attention_tiles.cu"
 
@@ -19,7 +23,8 @@ constexpr int PA_WARPS = 4;
 constexpr int PA_THREADS = (PA_WARPS + 1) * 32;
 constexpr int PA_ROWS = 16;
 
-template <int D, bool CODES>
+// NQ: products of eight query rows (1 or 2).
+template <int D, bool CODES, int NQ>
 struct RowsShape {
     static constexpr int SIZE = CODES ? 1 : 2;                         // bytes of an element
     static constexpr int ROW = D * SIZE;                               // bytes of a key
@@ -29,10 +34,13 @@ struct RowsShape {
     static constexpr int HALF = KT * ROW;                              // bytes of a tile's keys (or values)
     static constexpr int STEPS = CODES ? KT * 4 : 0;                   // bytes of a tile's key (or value) steps
     static constexpr int STAGE = 2 * HALF;
-    static constexpr int STAGES = STAGE == 32768 ? 3 : 5;
-    static constexpr int PART = 16 * D + 32;                           // floats of a partial result: a warp's output fragments [D/2][32], maxima [16], sums [16]
+    static constexpr int CTAS = NQ == 1 ? 3 : 2;                       // on an SM
+    static constexpr int STAGES = (NQ == 1 ? 2 : 3) * 32768 / STAGE + (CODES && NQ == 2 ? -1 : 0);
+    static constexpr int NREG = NQ * D / 4;                            // a thread's outputs
+    static constexpr int PART = NREG * 32 + NQ * 16;                   // floats of a partial result: a warp's output fragments, maxima and sums of the rows
     static constexpr int MERGE = 2 * PART * 4;
     static constexpr int SMEM = STAGES * (STAGE + 2 * STEPS) + MERGE + 256;
+    static_assert(SMEM <= 233472 / CTAS - 1024, "shared memory");
 };
 
 struct RowsParams {
@@ -49,14 +57,14 @@ struct RowsParams {
 };
 
 template <typename T>
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+__device__ __forceinline__ void mma16816(float* d, const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <>
-__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816<__nv_bfloat16>(float* d, const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
-__device__ __forceinline__ void mma16816<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816<__half>(float* d, const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -65,6 +73,12 @@ __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// An 8 x 8 matrix of 16-bit elements in fragment form (row lane / 4, columns 2 (lane % 4) and the next), transposed.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
@@ -76,11 +90,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
 }
-
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
 __device__ __forceinline__ void consumer_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 // Joins two partial results of the same rows: (m, l, o) <- both.  A maximum of -inf stands for no key yet.
@@ -91,47 +100,62 @@ __device__ __forceinline__ void join_scales(float m, float other, float& top, fl
     theirs = exp2_approx(other - base);
 }
 
-// Writes a finished item's rows from their fragments.  o[4 j + 2 r + e]: row lane / 4 + 8 r of product j.
-template <int D, typename T, bool CODES>
-__device__ __forceinline__ void write_rows(const RowsParams& P, const Sequence& s, int h, int p, const float (&o)[D / 2], const float (&m)[2],
-                                           const float (&l)[2]) {
-    const int lane = threadIdx.x & 31, c = lane & 3;
-    const int tokens = min(P.plan.tile_tokens, s.queries - p * P.plan.tile_tokens), rows = tokens * P.plan.group;
+// Writes the finished columns (query rows 8 n + 2 (lane % 4) + e) of one product's outputs: o[4 * n + 2 * half + e] is channel 16 mt + lane / 4 + 8 half, with
+// codes (D / 8) (lane / 4) + 2 mt + half.
+template <int D, typename T, bool CODES, int NQ>
+__device__ __forceinline__ void write_product(const RowsParams& P, const Sequence& s, int h, int p, int mt, const float* o, const float (&inv)[NQ][2]) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3, i0 = p * P.plan.tile_tokens;
+    const int rows = min(P.plan.tile_tokens, s.queries - i0) * P.plan.group;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = (lane >> 2) + 8 * r;
-        if (row >= rows) continue;
-        const int i = row / P.plan.group, head = h * P.plan.group + row - i * P.plan.group;
-        const long long token = s.first + p * P.plan.tile_tokens + i;
-        const float inv = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
-        T* const to = (T*)P.out + token * P.out_token + head * P.out_head;
-        if (CODES) {                                                    // columns 2c * (D/8) + j and (2c + 1) * (D/8) + j
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int j = 0; j < D / 8; j += 8) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = pack16<T>(o[4 * (j + 2 * k) + 2 * r + e] * inv, o[4 * (j + 2 * k + 1) + 2 * r + e] * inv);
-                    *reinterpret_cast<uint4*>(to + (2 * c + e) * (D / 8) + j) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-        } else {                                                        // columns 8 j + 2c, 8 j + 2c + 1
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j)
-                *reinterpret_cast<uint32_t*>(to + 8 * j + 2 * c) = pack16<T>(o[4 * j + 2 * r] * inv, o[4 * j + 2 * r + 1] * inv);
+    for (int n = 0; n < NQ; ++n) {
+        // transposed: row 8 n + g, the matrix rows 2c and 2c + 1 of both halves
+        const uint32_t a = transpose8x8(pack16<T>(o[4 * n] * inv[n][0], o[4 * n + 1] * inv[n][1]));
+        const uint32_t b = transpose8x8(pack16<T>(o[4 * n + 2] * inv[n][0], o[4 * n + 3] * inv[n][1]));
+        const int row = 8 * n + g;
+        if (row < rows) {
+            const int i = row / P.plan.group, head = h * P.plan.group + row - i * P.plan.group;
+            T* const to = (T*)P.out + (long long)(s.first + i0 + i) * P.out_token + head * P.out_head;
+            if (CODES) {
+                *reinterpret_cast<uint32_t*>(to + (D / 8) * (2 * c) + 2 * mt) = __byte_perm(a, b, 0x5410);
+                *reinterpret_cast<uint32_t*>(to + (D / 8) * (2 * c + 1) + 2 * mt) = __byte_perm(a, b, 0x7632);
+            } else {
+                *reinterpret_cast<uint32_t*>(to + 16 * mt + 2 * c) = a;
+                *reinterpret_cast<uint32_t*>(to + 16 * mt + 8 + 2 * c) = b;
+            }
         }
-        if (P.lse && c == 0) P.lse[token * P.q_heads + head] = l[r] > 0.0f ? (m[r] + log2f(l[r])) * 0.69314718055994531f : -INFINITY;
+        __syncwarp();
     }
 }
+template <int NQ>
+__device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s, int h, int p, const float (&m)[NQ][2], const float (&l)[NQ][2]) {
+    const int lane = threadIdx.x & 31, i0 = p * P.plan.tile_tokens, rows = min(P.plan.tile_tokens, s.queries - i0) * P.plan.group;
+    if (!P.lse || lane >= 4) return;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = 8 * n + 2 * lane + e;
+            if (row >= rows) continue;
+            const int i = row / P.plan.group, head = h * P.plan.group + row - i * P.plan.group;
+            P.lse[(long long)(s.first + i0 + i) * P.q_heads + head] = l[n][e] > 0.0f ? (m[n][e] + log2f(l[n][e])) * 0.69314718055994531f : -INFINITY;
+        }
+}
 
-template <int D, typename T, bool CODES>
-__global__ void __launch_bounds__(PA_THREADS, 2)
+template <int D, typename T, bool CODES, int NQ>
+__global__ void __launch_bounds__(PA_THREADS, RowsShape<D, CODES, NQ>::CTAS)
 paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ RowsParams P) {
-    using S = RowsShape<D, CODES>;
-    constexpr int KT = S::KT, NK = S::NK, STAGES = S::STAGES, NT = NK / 8;
-    // Probabilities times steps enter the second contraction in the queries' type.  In fp16 they would run out of exponents, so they are
-    // taken relative to the largest step so far (its power of two).
-    constexpr bool SCALED = CODES && std::is_same<T, __half>::value;
+    using S = RowsShape<D, CODES, NQ>;
+    using Runs = QueryRuns<S::KT>;
+    constexpr int KT = S::KT, NK = S::NK, STAGES = S::STAGES, NU = NK / 16;
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+    // Codes: queries in bf16 are brought to fp16 as multiples of a power of two for each row (exact for all that is within 2^-29 of the row's
+    // largest).  Probabilities times value steps enter the second contraction in fp16 too, relative to the largest step so far (its power of two), so
+    // that they do not run out of exponents.
+    constexpr bool RESCALED_Q = CODES && BF16;
+    using M = typename std::conditional<CODES, __half, T>::type;       // operands' type
+    // A second product with what the first one's rounding left, except where the output is rounded eight times as coarsely, and where the
+    // products would set the pace (two columns of products: 2 x 131,072 keys, twelve rows, 101 -> 121 us).
+    constexpr bool SPLIT = NQ == 1 && !(CODES && BF16);
     extern __shared__ __align__(1024) uint8_t pa_smem[];
     const uint32_t smem = ptx::smem_addr(pa_smem);
     const uint32_t steps0 = smem + STAGES * S::STAGE;                  // [stage][keys, values][KT]
@@ -155,7 +179,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     grid_dependency_launch();
     if (warp == 0) {
         bool bad = false;
-        const Stretch r = plan_stretch<QueryRuns<KT>>(P.plan, blockIdx.x, gridDim.x, bad);
+        const Stretch r = plan_stretch<Runs>(P.plan, blockIdx.x, gridDim.x, bad);
         if (lane == 0) {
             *shared_stretch = r;
             P.notes[blockIdx.x] = join_note(r, blockIdx.x);
@@ -163,7 +187,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
     }
     __syncthreads();
-    StretchWalk<QueryRuns<KT>> w;
+    StretchWalk<Runs> w;
     w.begin(P.plan, *shared_stretch);
     bool ok = true;
     int stage = 0;
@@ -173,17 +197,21 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     };
 
     if (warp == PA_WARPS) {
-        // ---- producer: lane r copies the tile's r-th run of page rows ----------------------------------------------------
+        // ---- producer: lane r copies the tile's r-th run of page rows; its page is looked up a tile ahead ----------------------
         const int copies = KT / P.page_rows, copy_bytes = P.page_rows * S::ROW;
         const int page_mask = (1 << P.plan.seq.page_shift) - 1;
         int issued = 0;
         for (; ok && w.more(); w.next(P.plan)) {
-            for (int t = w.tile; t < w.end; ++t) {
+            auto page_at = [&](int t) {
                 const int key = w.first + t * KT + lane * P.page_rows;
-                const bool mine = lane < copies && key < w.s.length;
-                const int page = mine ? page_of(P.plan.seq, w.b, key) : 0;
-                const bool inside = mine && page < P.plan.seq.pages;
+                return lane < copies && t < w.end && key < w.s.length ? page_of(P.plan.seq, w.b, key) : -1;
+            };
+            int next = page_at(w.tile);
+            for (int t = w.tile; t < w.end; ++t) {
+                const int key = w.first + t * KT + lane * P.page_rows, page = next;
+                const bool mine = page >= 0, inside = mine && page < P.plan.seq.pages;
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, mine)), n_steps = __popc(__ballot_sync(0xffffffffu, inside));
+                next = page_at(t + 1);
                 ok = mbar_wait_warp(bars + 8 * (STAGES + stage), phase ^ 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t full = bars + 8 * stage;
@@ -217,38 +245,79 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
     // ---- four warps, a quarter of every tile's keys each ------------------------------------------------------------------
     const int g = lane >> 2, c = lane & 3, rows_shift = 31 - __clz(P.page_rows);
-    const float sc = P.c;
+    // where the warp's sixteen keys lie in a tile (each in one page)
+    uint32_t group_at[NU];
+    int in_block[NU];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        const int j = warp * NK + 16 * u;
+        group_at[u] = (j >> rows_shift) * (P.page_rows * S::ROW);
+        in_block[u] = j & (P.page_rows - 1);
+    }
     while (w.more()) {
         const int i0 = w.p * P.plan.tile_tokens, tokens = min(P.plan.tile_tokens, w.s.queries - i0), rows = tokens * P.plan.group;
         const int base = w.s.length - w.s.queries + i0;                  // position of the item's first token
-        // queries as the left operand: rows g and g + 8
-        uint32_t qa[D / 16][4];
-        int low[2], high[2];                                             // the keys that the two rows see
+        // queries as the right operand: column 8 n + g
+        uint32_t qb[NQ][D / 16][2];
+        float sc[NQ][2];                                                 // scale of the thread's score columns 2c and 2c + 1
+        int low[NQ][2], high[NQ][2];                                     // the keys that they see
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int row = g + 8 * r, i = row / P.plan.group;
+        for (int n = 0; n < NQ; ++n) {
+            const int row = 8 * n + g, i = row / P.plan.group;
             const bool live = row < rows;
             const T* const from = (const T*)P.q + (long long)(w.s.first + i0 + i) * P.q_token + (long long)(w.h * P.plan.group + row - i * P.plan.group) * P.q_head;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 if (CODES) {                                             // channels as the codes lie: 16 (c + 4 (k / 4)) + 4 (k % 4) + 0 .. 3
                     const uint2 v = live ? *reinterpret_cast<const uint2*>(from + 16 * (c + 4 * (k >> 2)) + 4 * (k & 3)) : make_uint2(0u, 0u);
-                    qa[k][r] = v.x;
-                    qa[k][2 + r] = v.y;
+                    qb[n][k][0] = v.x;
+                    qb[n][k][1] = v.y;
                 } else {
-                    qa[k][r] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 2 * c) : 0u;
-                    qa[k][2 + r] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 8 + 2 * c) : 0u;
+                    qb[n][k][0] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 2 * c) : 0u;
+                    qb[n][k][1] = live ? *reinterpret_cast<const uint32_t*>(from + 16 * k + 8 + 2 * c) : 0u;
                 }
             }
-            high[r] = !live ? 0 : P.plan.causal ? min(base + i + 1, w.s.length) : w.s.length;
-            low[r] = P.plan.window ? base + i - P.plan.window + 1 : 0;
+            float unscale = P.c;
+            if (RESCALED_Q) {
+                uint32_t largest = 0;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) largest = max(largest, max((qb[n][k][e] & 0x7FFFu) << 16, qb[n][k][e] & 0x7FFF0000u));
+                largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 1));
+                largest = max(largest, __shfl_xor_sync(0xffffffffu, largest, 2));
+                // the largest becomes 2^14 .. 2^15; 2^x for x within the exponents' range on both sides
+                const int shift = min(max(141 - (int)(largest >> 23), -110), 110);
+                const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+                unscale = P.c * __uint_as_float((uint32_t)(127 - shift) << 23);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float2 f = unpack16<T>(qb[n][k][e]);
+                        qb[n][k][e] = pack16<__half>(f.x * up, f.y * up);
+                    }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sc[n][e] = RESCALED_Q ? __shfl_sync(0xffffffffu, unscale, (2 * c + e) * 4) : P.c;
+                const int mine = 8 * n + 2 * c + e, token = mine / P.plan.group;
+                high[n][e] = mine >= rows ? 0 : P.plan.causal ? min(base + token + 1, w.s.length) : w.s.length;
+                low[n][e] = P.plan.window ? base + token - P.plan.window + 1 : 0;
+            }
         }
         const int all_low = P.plan.window ? base + tokens - P.plan.window : 0;                               // the last row's
         const int all_high = P.plan.causal ? min(base + 1, w.s.length) : w.s.length;                         // the first row's
-        float o[D / 2], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-        uint32_t unit = 0x00800000u;                                     // SCALED: the power of two that o is a multiple of
+        float o[D / 16][4 * NQ], m[NQ][2], l[NQ][2];
+        uint32_t unit = 0x00800000u;                                     // CODES: the power of two that o is a multiple of
 #pragma unroll
-        for (int i = 0; i < D / 2; ++i) o[i] = 0.0f;
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4 * NQ; ++e) o[i][e] = 0.0f;
 
         for (int t = w.tile; t < w.end; ++t) {
             ok = ok && mbar_wait_warp(bars + 8 * stage, phase, abort_flag);
@@ -256,127 +325,151 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 const uint32_t kbase = smem + stage * S::STAGE;
                 const int key0 = w.first + t * KT + warp * NK;
                 const bool edge = key0 < all_low || key0 + NK > all_high;
-                float s[NT][4];
+                float s[NU][4 * NQ];
 #pragma unroll
-                for (int u = 0; u < NK / 16; ++u) {                      // sixteen keys, in one page
-                    const int j = warp * NK + 16 * u, block = j >> rows_shift, in_block = j & (P.page_rows - 1);
-                    const uint32_t at = kbase + block * (P.page_rows * S::ROW);
+                for (int u = 0; u < NU; ++u) {                           // sixteen keys
+                    const uint32_t at = kbase + group_at[u];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[2 * u][e] = s[2 * u + 1][e] = 0.0f;
+                    for (int e = 0; e < 4 * NQ; ++e) s[u][e] = 0.0f;
                     if (!CODES) {
-                        const int row = in_block + (lane >> 4) * 8 + (lane & 7), odd = (lane >> 3) & 1;
+                        const int row = in_block[u] + ((lane >> 3) & 1) * 8 + (lane & 7), odd = lane >> 4;
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
                             const int chunk = 2 * k + odd;
-                            uint32_t b[4];
-                            ldmatrix4(at + (chunk >> 3) * (P.page_rows * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), b);
-                            mma16816<T>(s[2 * u], qa[k], b[0], b[1]);
-                            mma16816<T>(s[2 * u + 1], qa[k], b[2], b[3]);
+                            uint32_t a[4];
+                            ldmatrix4(at + (chunk >> 3) * (P.page_rows * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), a);
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) mma16816<M>(&s[u][4 * n], a, qb[n][k][0], qb[n][k][1]);
                         }
                     } else {
+                        const int row = in_block[u] + g;                 // and row + 8, whose swizzle is the same
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const int row = in_block + 8 * half + g;
+                        for (int x = 0; x < D / 64; ++x) {
+                            const uint32_t chunk = c + 4 * x;
+                            const uint32_t from = at + row * S::LINE + ((S::LINE == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4);
+                            const uint4 v0 = lds128(from), v1 = lds128(from + 8 * S::LINE);
+                            const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
-                            for (int x = 0; x < D / 64; ++x) {
-                                const uint32_t chunk = c + 4 * x;
-                                const uint4 v = lds128(at + row * S::LINE + ((S::LINE == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4));
-                                const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+                            for (int k = 0; k < 4; ++k) {
+                                const uint2 e0 = codes_to_half4(w0[k]), e1 = codes_to_half4(w1[k]);
+                                const uint32_t a[4] = {e0.x, e1.x, e0.y, e1.y};
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    mma16816<T>(s[2 * u + half], qa[4 * x + k], codes_to_16<T>(__byte_perm(words[k], 0u, 0x4140)),
-                                                codes_to_16<T>(__byte_perm(words[k], 0u, 0x4342)));
+                                for (int n = 0; n < NQ; ++n) mma16816<M>(&s[u][4 * n], a, qb[n][4 * x + k][0], qb[n][4 * x + k][1]);
                             }
                         }
                     }
                 }
-                // scores in units of log2, hidden ones -inf, and the rows' maxima
-                const float* const ks = reinterpret_cast<const float*>(pa_smem + STAGES * S::STAGE + stage * 2 * S::STEPS) + warp * NK;
+                // scores in units of log2, hidden ones -inf, and the columns' maxima.  s[u][4 n + 2 r + e]: key 16 u + g + 8 r, column 8 n + 2c + e
+                const float* const ks = reinterpret_cast<const float*>(pa_smem + STAGES * S::STAGE + stage * 2 * S::STEPS) + warp * NK + g;
                 const float* const vs = ks + KT;
-                float top[2] = {m[0], m[1]};
+                float top[NQ][2];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float2 f = make_float2(sc, sc);
-                    if (CODES) {
-                        f = *reinterpret_cast<const float2*>(ks + 8 * n + 2 * c);
-                        f.x *= sc;
-                        f.y *= sc;
+                for (int n = 0; n < NQ; ++n) { top[n][0] = m[n][0]; top[n][1] = m[n][1]; }
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float step = CODES ? ks[16 * u + 8 * r] : 1.0f;
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float& x = s[u][4 * n + 2 * r + e];
+                                x *= CODES ? sc[n][e] * step : sc[n][e];
+                                if (edge) {
+                                    const int key = key0 + 16 * u + 8 * r + g;
+                                    if (key < low[n][e] || key >= high[n][e]) x = -INFINITY;
+                                }
+                                top[n][e] = fmaxf(top[n][e], x);
+                            }
                     }
+                bool grew = false;
+                float from[NQ][2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[n][e] *= (e & 1) ? f.y : f.x;
-                        if (edge) {
-                            const int key = key0 + 8 * n + 2 * c + (e & 1);
-                            if (key < low[e >> 1] || key >= high[e >> 1]) s[n][e] = -INFINITY;
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], x));
+                        from[n][e] = top[n][e] == -INFINITY ? 0.0f : top[n][e];
+                        grew = grew || top[n][e] != m[n][e];
+                    }
+                if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float factor = exp2_approx(m[n][e] - from[n][e]);
+                            l[n][e] *= factor;
+                            m[n][e] = top[n][e];
+#pragma unroll
+                            for (int i = 0; i < D / 16; ++i) { o[i][4 * n + e] *= factor; o[i][4 * n + 2 + e] *= factor; }
                         }
-                        top[e >> 1] = fmaxf(top[e >> 1], s[n][e]);
-                    }
-                }
-                float factor[2], from[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-                    from[r] = top[r] == -INFINITY ? 0.0f : top[r];
-                    factor[r] = exp2_approx(m[r] - from[r]);
-                }
-                if (__any_sync(0xffffffffu, top[0] != m[0] || top[1] != m[1])) {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) { l[r] *= factor[r]; m[r] = top[r]; }
-#pragma unroll
-                    for (int i = 0; i < D / 2; ++i) o[i] *= factor[(i >> 1) & 1];
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int u = 0; u < NU; ++u)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[n][e] = exp2_approx(s[n][e] - from[e >> 1]);
-                        l[e >> 1] += s[n][e];
-                    }
-                if (SCALED) {
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float& x = s[u][4 * n + e];
+                            x = exp2_approx(x - from[n][e & 1]);
+                            l[n][e & 1] += x;
+                        }
+                if (CODES) {
+                    float step[NU][2];
                     uint32_t largest = unit;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint2 f = *reinterpret_cast<const uint2*>(vs + 8 * n + 2 * c);
-                        const int key = key0 + 8 * n + 2 * c;
-                        if (!edge || key < w.s.length) largest = max(largest, f.x & 0x7F800000u);
-                        if (!edge || key + 1 < w.s.length) largest = max(largest, f.y & 0x7F800000u);
-                    }
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            step[u][r] = vs[16 * u + 8 * r];
+                            if (edge && key0 + 16 * u + 8 * r + g >= w.s.length) step[u][r] = 0.0f;      // (behind the length: whatever lies there)
+                            largest = max(largest, __float_as_uint(step[u][r]) & 0x7F800000u);
+                        }
                     largest = min(__reduce_max_sync(0xffffffffu, largest), 0x7E000000u);
                     if (largest != unit) {
                         const float down = __uint_as_float(0x3F800000u - min(largest - unit, 0x3F000000u));
 #pragma unroll
-                        for (int i = 0; i < D / 2; ++i) o[i] *= down;
+                        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4 * NQ; ++e) o[i][e] *= down;
                         unit = largest;
                     }
-                }
-                // outputs: the probabilities of sixteen keys are the left operand as they are
+                    const float up = __uint_as_float(0x7F000000u - unit);                                   // 1 / unit
 #pragma unroll
-                for (int u = 0; u < NK / 16; ++u) {
-                    const int j = warp * NK + 16 * u, block = j >> rows_shift, in_block = j & (P.page_rows - 1);
-                    const uint32_t at = kbase + S::HALF + block * (P.page_rows * S::ROW);
-                    if (CODES) {
+                    for (int u = 0; u < NU; ++u)
 #pragma unroll
-                        for (int n = 2 * u; n < 2 * u + 2; ++n) {
-                            float2 f = *reinterpret_cast<const float2*>(vs + 8 * n + 2 * c);
-                            if (edge) {                                  // (places behind the length: whatever lies there)
-                                const int key = key0 + 8 * n + 2 * c;
-                                if (key >= w.s.length) f.x = 0.0f;
-                                if (key + 1 >= w.s.length) f.y = 0.0f;
-                            }
-                            if (SCALED) {
-                                const float up = __uint_as_float(0x7F000000u - unit);      // 1 / unit
-                                f.x *= up;
-                                f.y *= up;
-                            }
-                            s[n][0] *= f.x; s[n][1] *= f.y; s[n][2] *= f.x; s[n][3] *= f.y;
+                        for (int r = 0; r < 2; ++r) {
+                            const float f = step[u][r] * up;
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) { s[u][4 * n + 2 * r] *= f; s[u][4 * n + 2 * r + 1] *= f; }
                         }
-                    }
-                    uint32_t pa[4];
-                    pa[0] = pack16<T>(s[2 * u][0], s[2 * u][1]);
-                    pa[1] = pack16<T>(s[2 * u][2], s[2 * u][3]);
-                    pa[2] = pack16<T>(s[2 * u + 1][0], s[2 * u + 1][1]);
-                    pa[3] = pack16<T>(s[2 * u + 1][2], s[2 * u + 1][3]);
+                }
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    // probabilities as the right operand: columns 8 n + g, keys 2c, 2c + 1 and 8 further
+                    uint32_t pb[NQ][2], rest[NQ][2];
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float a = s[u][4 * n + 2 * r], b = s[u][4 * n + 2 * r + 1];
+                            const uint32_t first = pack16<M>(a, b);
+                            pb[n][r] = transpose8x8(first);
+                            if (SPLIT) {
+                                const float2 f = unpack16<M>(first);
+                                rest[n][r] = transpose8x8(pack16<M>(a - f.x, b - f.y));
+                            }
+                        }
+                    const uint32_t at = kbase + S::HALF + group_at[u];
+                    auto product = [&](int mt, const uint32_t (&a)[4]) {
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            mma16816<M>(&o[mt][4 * n], a, pb[n][0], pb[n][1]);
+                            if (SPLIT) mma16816<M>(&o[mt][4 * n], a, rest[n][0], rest[n][1]);
+                        }
+                    };
                     if (!CODES) {
                         uint32_t mask0 = 0xFFFFFFFFu, mask1 = 0xFFFFFFFFu;     // values behind the length are not multiplied: NaN times 0
                         if (edge) {
@@ -384,22 +477,21 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             mask0 = (key < w.s.length ? 0xFFFFu : 0u) | (key + 1 < w.s.length ? 0xFFFF0000u : 0u);
                             mask1 = (key + 8 < w.s.length ? 0xFFFFu : 0u) | (key + 9 < w.s.length ? 0xFFFF0000u : 0u);
                         }
-                        const int row = in_block + ((lane >> 3) & 1) * 8 + (lane & 7), odd = lane >> 4;
+                        const int row = in_block[u] + (lane >> 4) * 8 + (lane & 7), odd = (lane >> 3) & 1;
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const int chunk = 2 * k + odd;
-                            uint32_t b[4];
-                            ldmatrix4_trans(at + (chunk >> 3) * (P.page_rows * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), b);
-                            if (edge) { b[0] &= mask0; b[1] &= mask1; b[2] &= mask0; b[3] &= mask1; }
-                            mma16816<T>(*reinterpret_cast<float(*)[4]>(&o[8 * k]), pa, b[0], b[1]);
-                            mma16816<T>(*reinterpret_cast<float(*)[4]>(&o[8 * k + 4]), pa, b[2], b[3]);
+                        for (int mt = 0; mt < D / 16; ++mt) {
+                            const int chunk = 2 * mt + odd;
+                            uint32_t a[4];
+                            ldmatrix4_trans(at + (chunk >> 3) * (P.page_rows * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), a);
+                            if (edge) { a[0] &= mask0; a[1] &= mask0; a[2] &= mask1; a[3] &= mask1; }
+                            product(mt, a);
                         }
                     } else {
-                        // a thread's columns: D/8 codes of its four keys, which are the right operand of D/8 products
+                        // D/8 codes of four keys: the thread's channels (D/8) g + 0, 1, ...
                         uint32_t words[4][D / 32];
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            const int row = in_block + 2 * c + (x & 1) + 8 * (x >> 1);
+                            const int row = in_block[u] + 2 * c + (x & 1) + 8 * (x >> 1);
                             if (D == 128) {
                                 const uint4 v = lds128(at + row * 128 + ((g ^ (row & 7)) << 4));
                                 words[x][0] = v.x; words[x][1] = v.y; words[x][D / 32 - 2] = v.z; words[x][D / 32 - 1] = v.w;
@@ -409,11 +501,14 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             }
                         }
 #pragma unroll
-                        for (int n = 0; n < D / 8; ++n) {
-                            const uint32_t pick = (n & 3) | ((4 + (n & 3)) << 8);               // byte n % 4 of both words
-                            const uint32_t b0 = codes_to_16<T>(__byte_perm(words[0][n >> 2], words[1][n >> 2], pick));
-                            const uint32_t b1 = codes_to_16<T>(__byte_perm(words[2][n >> 2], words[3][n >> 2], pick));
-                            mma16816<T>(*reinterpret_cast<float(*)[4]>(&o[4 * n]), pa, b0, b1);
+                        for (int mt = 0; mt < D / 16; ++mt) {
+                            uint32_t a[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {                // channel 2 mt + r % 2, keys (r / 2) * 8 + 2c and the next
+                                const int j = 2 * mt + (r & 1), x = 2 * (r >> 1);
+                                a[r] = codes_to_16<__half>(__byte_perm(words[x][j >> 2], words[x + 1][j >> 2], (j & 3) | ((4 + (j & 3)) << 8)));
+                            }
+                            product(mt, a);
                         }
                     }
                 }
@@ -423,34 +518,51 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             advance();
         }
 
-        if (SCALED) {
+        if (CODES) {
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) o[i] *= __uint_as_float(unit);
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4 * NQ; ++e) o[i][e] *= __uint_as_float(unit);
         }
         // ---- the four warps' results become one (every warp passes these barriers, whatever became of its waits) -------------
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        }
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], x);
         auto put = [&](float* to) {
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) to[i * 32 + lane] = o[i];
+            for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-                if (c == 0) { to[16 * D + 8 * r + g] = m[r]; to[16 * D + 16 + 8 * r + g] = l[r]; }
+                for (int e = 0; e < 4 * NQ; ++e) to[(i * 4 * NQ + e) * 32 + lane] = o[i][e];
+            if (g == 0) {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        to[S::NREG * 32 + 8 * n + 2 * c + e] = m[n][e];
+                        to[S::NREG * 32 + 8 * (NQ + n) + 2 * c + e] = l[n][e];
+                    }
+            }
         };
         auto join = [&](const float* from) {
-            float mine[2], theirs[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float top;
-                join_scales(m[r], from[16 * D + 8 * r + g], top, mine[r], theirs[r]);
-                m[r] = top;
-                l[r] = l[r] * mine[r] + from[16 * D + 16 + 8 * r + g] * theirs[r];
-            }
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) o[i] = o[i] * mine[(i >> 1) & 1] + from[i * 32 + lane] * theirs[(i >> 1) & 1];
+                for (int e = 0; e < 2; ++e) {
+                    float top, mine, theirs;
+                    join_scales(m[n][e], from[S::NREG * 32 + 8 * n + 2 * c + e], top, mine, theirs);
+                    m[n][e] = top;
+                    l[n][e] = l[n][e] * mine + from[S::NREG * 32 + 8 * (NQ + n) + 2 * c + e] * theirs;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            float& x = o[i][4 * n + 2 * r + e];
+                            x = x * mine + from[(i * 4 * NQ + 4 * n + 2 * r + e) * 32 + lane] * theirs;
+                        }
+                }
         };
         consumer_barrier();                                              // the last item's results have been read
         if (warp >= 2) put(merge + (warp - 2) * S::PART);
@@ -461,99 +573,91 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         consumer_barrier();
         if (warp == 0) {
             join(merge + S::PART);
-            if (ok) {
-                if (w.whole()) write_rows<D, T, CODES>(P, w.s, w.h, w.p, o, m, l);
-                else put(P.partial + (2ll * blockIdx.x + (w.tile > 0 ? 0 : 1)) * S::PART);
+            if (ok && w.whole()) {
+                float inv[NQ][2];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) inv[n][e] = l[n][e] > 0.0f ? 1.0f / l[n][e] : 0.0f;
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt) write_product<D, T, CODES, NQ>(P, w.s, w.h, w.p, mt, o[mt], inv);
+                write_lse<NQ>(P, w.s, w.h, w.p, m, l);
+            } else if (ok) {
+                put(P.partial + (2ll * blockIdx.x + (w.tile > 0 ? 0 : 1)) * S::PART);
             }
         }
         w.next(P.plan);
     }
 }
 
-// Joins the partial results of an item that several CTAs worked on: the block of the second of them does it.  Eight warps
-// take an eighth of the outputs each.
-template <int D, typename T, bool CODES>
-__global__ void __launch_bounds__(256)
+// Joins the partial results of an item that several CTAs worked on: the block of the second of them does it, a warp for every product.
+template <int D, typename T, bool CODES, int NQ>
+__global__ void __launch_bounds__(D * 2)
 paged_rows_join_kernel(const __grid_constant__ RowsParams P) {
-    using S = RowsShape<D, CODES>;
-    constexpr int SHARE = D / 16;
+    using S = RowsShape<D, CODES, NQ>;
     grid_dependency_wait();
     grid_dependency_launch();
-    const JoinNote n = P.notes[blockIdx.x + 1];
-    if (n.last_cta < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2;
-    float o[SHARE], m[2], l[2];
-    const float* at = P.partial + (2ll * n.first_cta + 1) * S::PART ;
+    const JoinNote note = P.notes[blockIdx.x + 1];
+    if (note.last_cta < 0) return;
+    const int mt = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 3;
+    float o[4 * NQ], m[NQ][2], l[NQ][2];
 #pragma unroll
-    for (int i = 0; i < SHARE; ++i) o[i] = at[(warp * SHARE + i) * 32 + lane];
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-    for (int r = 0; r < 2; ++r) { m[r] = at[16 * D + 8 * r + g]; l[r] = at[16 * D + 16 + 8 * r + g]; }
+        for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
+#pragma unroll
+    for (int e = 0; e < 4 * NQ; ++e) o[e] = 0.0f;
 #pragma unroll 4
-    for (int cta = n.first_cta + 1; cta <= n.last_cta; ++cta) {
-        at = P.partial + 2ll * cta * S::PART ;
-        float mine[2], theirs[2];
+    for (int cta = note.first_cta; cta <= note.last_cta; ++cta) {
+        const float* const at = P.partial + (2ll * cta + (cta == note.first_cta ? 1 : 0)) * S::PART;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float top;
-            join_scales(m[r], at[16 * D + 8 * r + g], top, mine[r], theirs[r]);
-            m[r] = top;
-            l[r] = l[r] * mine[r] + at[16 * D + 16 + 8 * r + g] * theirs[r];
-        }
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-        for (int i = 0; i < SHARE; ++i) o[i] = o[i] * mine[(i >> 1) & 1] + at[(warp * SHARE + i) * 32 + lane] * theirs[(i >> 1) & 1];
-    }
-    const Sequence s = sequence_of(P.plan.seq, n.b);
-    const int c = lane & 3, i0 = n.p * P.plan.tile_tokens, rows = min(P.plan.tile_tokens, s.queries - i0) * P.plan.group;
+            for (int e = 0; e < 2; ++e) {
+                float top, mine, theirs;
+                join_scales(m[n][e], at[S::NREG * 32 + 8 * n + 2 * c + e], top, mine, theirs);
+                m[n][e] = top;
+                l[n][e] = l[n][e] * mine + at[S::NREG * 32 + 8 * (NQ + n) + 2 * c + e] * theirs;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        const int row = g + 8 * r;
-        if (row >= rows) continue;
-        const int i = row / P.plan.group, head = n.h * P.plan.group + row - i * P.plan.group;
-        const long long token = s.first + i0 + i;
-        const float inv = l[r] > 0.0f ? 1.0f / l[r] : 0.0f;
-        T* const to = (T*)P.out + token * P.out_token + head * P.out_head;
-#pragma unroll
-        for (int k = 0; k < SHARE / 4; ++k) {                             // product j: columns as in write_rows
-            const int j = warp * (SHARE / 4) + k;
-            const float a = o[4 * k + 2 * r] * inv, b = o[4 * k + 2 * r + 1] * inv;
-            if (CODES) {
-                const uint32_t w = pack16<T>(a, b);
-                reinterpret_cast<uint16_t*>(to)[2 * c * (D / 8) + j] = (uint16_t)w;
-                reinterpret_cast<uint16_t*>(to)[(2 * c + 1) * (D / 8) + j] = (uint16_t)(w >> 16);
-            } else {
-                *reinterpret_cast<uint32_t*>(to + 8 * j + 2 * c) = pack16<T>(a, b);
+                for (int r = 0; r < 2; ++r) o[4 * n + 2 * r + e] = o[4 * n + 2 * r + e] * mine + at[(mt * 4 * NQ + 4 * n + 2 * r + e) * 32 + lane] * theirs;
             }
-        }
-        if (P.lse && c == 0 && warp == 0) P.lse[token * P.q_heads + head] = l[r] > 0.0f ? (m[r] + log2f(l[r])) * 0.69314718055994531f : -INFINITY;
     }
+    const Sequence s = sequence_of(P.plan.seq, note.b);
+    float inv[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) inv[n][e] = l[n][e] > 0.0f ? 1.0f / l[n][e] : 0.0f;
+    write_product<D, T, CODES, NQ>(P, s, note.h, note.p, mt, o, inv);
+    if (mt == 0) write_lse<NQ>(P, s, note.h, note.p, m, l);
 }
 
-inline int rows_grid() { return 2 * sm_count(); }
-inline size_t rows_partial_bytes(int ctas, int head_dim) { return (size_t)ctas * 2 * (16 * head_dim + 32) * 4; }
+inline int rows_grid(int nq) { return (nq == 1 ? 3 : 2) * sm_count(); }
+inline size_t rows_partial_bytes(int nq, int head_dim) { return (size_t)rows_grid(nq) * 2 * (nq * head_dim * 8 + nq * 16) * 4; }
 
-template <int D, typename T, bool CODES>
+template <int D, typename T, bool CODES, int NQ>
 int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cache_batch* batch, void* workspace, cudaStream_t st) {
-    using S = RowsShape<D, CODES>;
+    using S = RowsShape<D, CODES, NQ>;
     CUtensorMap map_k, map_v;
     P.page_rows = cache->page_tokens < S::KT ? cache->page_tokens : S::KT;
     if (!encode_cache_map(&map_k, cache, cache->k, P.page_rows, true) || !encode_cache_map(&map_v, cache, cache->v, P.page_rows, true)) return VITINT_ERR_CUDA;
     const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + S::KT - 1) / S::KT;
     const long long items = (long long)batch->sequences * cache->kv_heads * runs;
     if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
-    int grid = rows_grid();
+    int grid = rows_grid(NQ);
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
-    P.partial = (float*)((uint8_t*)workspace + notes_bytes(rows_grid()));
+    P.partial = (float*)((uint8_t*)workspace + notes_bytes(rows_grid(NQ)));
     const int dev = current_device();
     if (dev < 0) return VITINT_ERR_CUDA;
     static bool attr_set_dev[MAX_DEVICES] = {};
     if (!attr_set_dev[dev]) {
-        if (cudaFuncSetAttribute(paged_rows_kernel<D, T, CODES>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return VITINT_ERR_CUDA;
+        if (cudaFuncSetAttribute(paged_rows_kernel<D, T, CODES, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) != cudaSuccess) return VITINT_ERR_CUDA;
         attr_set_dev[dev] = true;
     }
-    launch_kernel(paged_rows_kernel<D, T, CODES>, dim3(grid), dim3(PA_THREADS), S::SMEM, st, map_k, map_v, P);
+    launch_kernel(paged_rows_kernel<D, T, CODES, NQ>, dim3(grid), dim3(PA_THREADS), S::SMEM, st, map_k, map_v, P);
     if (int rc = cuda_status(cudaGetLastError())) return rc;
-    if (tiles > 1 && grid > 1) launch_kernel(paged_rows_join_kernel<D, T, CODES>, dim3(grid - 1), dim3(256), 0, st, P);
+    if (tiles > 1 && grid > 1) launch_kernel(paged_rows_join_kernel<D, T, CODES, NQ>, dim3(grid - 1), dim3(D * 2), 0, st, P);
     return cuda_status(cudaGetLastError());
 }
 
@@ -561,6 +665,9 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
 // paged_attention_tiles.cu.
 inline bool few_rows(int q_heads, const vitint_cache* cache, const vitint_cache_batch* batch) {
     return (int64_t)batch->max_queries * (q_heads / cache->kv_heads) <= PA_ROWS;
+}
+inline int row_products(int q_heads, const vitint_cache* cache, const vitint_cache_batch* batch) {
+    return batch->max_queries * (q_heads / cache->kv_heads) <= 8 ? 1 : 2;
 }
 
 }  // namespace
@@ -570,7 +677,10 @@ using namespace vitint;
 
 extern "C" size_t vitint_paged_attention_workspace_bytes(int32_t q_heads, const vitint_cache* cache, const vitint_cache_batch* batch) {
     if (check_cache(cache) != VITINT_OK || check_batch(cache, batch, true) != VITINT_OK || q_heads <= 0 || q_heads % cache->kv_heads != 0) return 0;
-    if (few_rows(q_heads, cache, batch)) return notes_bytes(rows_grid()) + rows_partial_bytes(rows_grid(), cache->head_dim);
+    if (few_rows(q_heads, cache, batch)) {
+        const int nq = row_products(q_heads, cache, batch);
+        return notes_bytes(rows_grid(nq)) + rows_partial_bytes(nq, cache->head_dim);
+    }
     return notes_bytes(sm_count()) + tiles_partial_bytes(sm_count(), cache->head_dim);
 }
 
@@ -613,11 +723,19 @@ extern "C" int vitint_paged_attention(const void* q, int32_t q_type, int64_t tok
     P.q_token = q_token_stride; P.q_head = q_head_stride; P.out_token = out_token_stride; P.out_head = out_head_stride;
     P.q_heads = q_heads;
     P.c = (float)((double)scale * 1.4426950408889634);
-    auto go = [&](auto launch) { return launch(P, cache, batch, workspace, st); };
+    auto go = [&](auto one, auto two) {
+        return row_products(q_heads, cache, batch) == 1 ? one(P, cache, batch, workspace, st) : two(P, cache, batch, workspace, st);
+    };
     if (cache->head_dim == 64) {
-        if (codes) return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, true>) : go(paged_rows_launch<64, __half, true>);
-        return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, false>) : go(paged_rows_launch<64, __half, false>);
+        if (codes)
+            return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, true, 1>, paged_rows_launch<64, __nv_bfloat16, true, 2>)
+                        : go(paged_rows_launch<64, __half, true, 1>, paged_rows_launch<64, __half, true, 2>);
+        return bf16 ? go(paged_rows_launch<64, __nv_bfloat16, false, 1>, paged_rows_launch<64, __nv_bfloat16, false, 2>)
+                    : go(paged_rows_launch<64, __half, false, 1>, paged_rows_launch<64, __half, false, 2>);
     }
-    if (codes) return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, true>) : go(paged_rows_launch<128, __half, true>);
-    return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, false>) : go(paged_rows_launch<128, __half, false>);
+    if (codes)
+        return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, true, 1>, paged_rows_launch<128, __nv_bfloat16, true, 2>)
+                    : go(paged_rows_launch<128, __half, true, 1>, paged_rows_launch<128, __half, true, 2>);
+    return bf16 ? go(paged_rows_launch<128, __nv_bfloat16, false, 1>, paged_rows_launch<128, __nv_bfloat16, false, 2>)
+                : go(paged_rows_launch<128, __half, false, 1>, paged_rows_launch<128, __half, false, 2>);
 }

@@ -137,11 +137,6 @@ __device__ __forceinline__ void tile_probabilities(const uint32_t (&v)[32], cons
     }
 }
 
-__device__ __forceinline__ void tiles_bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
-}
-
 template <int D, typename T, bool CODES>
 __global__ void __launch_bounds__(TilesShape<D, CODES>::THREADS, 1)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -149,7 +144,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using S = TilesShape<D, CODES>;
     using Runs = QueryRuns<PT_KEYS>;
     constexpr int LINES = S::LINES;
-    constexpr bool SCALED = CODES && std::is_same<T, __half>::value;    // see paged_rows_kernel
+    // Codes: probabilities times value steps enter the second product in fp16, relative to the largest step so far (its power of two).
+    constexpr bool SCALED = CODES;
+    using M = typename std::conditional<CODES, __half, T>::type;        // the second product's type
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t O_COL = 256;                                     // tensor memory: S and P of the halves at 0 and 128, O at 256 and 256 + D
     extern __shared__ __align__(1024) uint8_t pt_smem[];
@@ -245,8 +242,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     __syncwarp();
                     if (inside) {
                         const long long at = (((long long)here * P.plan.kv_heads + w.h) << P.plan.seq.page_shift) + (key & page_mask);
-                        tiles_bulk_copy(to, P.k_steps + at, P.page_rows * 4, bar);
-                        tiles_bulk_copy(to + PT_KEYS * 4, P.v_steps + at, P.page_rows * 4, bar);
+                        bulk_copy(to, P.k_steps + at, P.page_rows * 4, bar);
+                        bulk_copy(to + PT_KEYS * 4, P.v_steps + at, P.page_rows * 4, bar);
                     }
                     __syncwarp();
                     ++steps_issued;
@@ -289,7 +286,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- products: P V of a tile and Q K^T of the next, one half after the other ------------------------------------------
         TileRing r;                                                     // the next entry of the ring: keys of the first tile, values, keys, ...
         uint32_t items = 0, n_p[2] = {0, 0};
-        const uint32_t idesc_qk = ptx::idesc_f16(128, PT_KEYS, BF16, 0), idesc_pv = ptx::idesc_f16(128, D, BF16, 1);
+        const uint32_t idesc_qk = ptx::idesc_f16(128, PT_KEYS, BF16, 0), idesc_pv = ptx::idesc_f16(128, D, std::is_same<M, __nv_bfloat16>::value, 1);
         auto issue_qk = [&](int x, int at) {
             const uint64_t a = ptx::smem_desc(smem + x * S::OPERAND, 16, 1024, ptx::SWIZZLE_128B);
             const uint64_t b = ptx::smem_desc(ring + at * S::OPERAND, 16, 1024, ptx::SWIZZLE_128B);
@@ -377,7 +374,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ok = mbar_wait_warp(ptx::smem_addr(&B.raw_full[raw.at]), raw.phase, abort_ptr) &&
                      mbar_wait_warp(ptx::smem_addr(&B.empty[slot.at]), slot.phase ^ 1u, abort_ptr);
                 if (!ok) break;
-                expand_code_row<D, T>(gen + (raw_ring - smem) + raw.at * S::RAW, gen + 2 * S::OPERAND + slot.at * S::OPERAND, row);
+                const uint8_t* const from = gen + (raw_ring - smem) + raw.at * S::RAW;
+                uint8_t* const to = gen + 2 * S::OPERAND + slot.at * S::OPERAND;
+                if (i & 1) expand_code_row<D, __half>(from, to, row);   // values
+                else expand_code_row<D, T>(from, to, row);
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -466,8 +466,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         ptx::tmem_ld_wait();
                         if (k < 3) ptx::tmem_ld32(t_s + 32 * (k + 1), v[(k + 1) & 1]);
                         uint32_t p[16];
-                        if (edge) tile_probabilities<T, CODES, true>(v[k & 1], f + 32 * k, up, c2, minus_base, lo - 32 * k, hi - 32 * k, sum, p);
-                        else tile_probabilities<T, CODES, false>(v[k & 1], f + 32 * k, up, c2, minus_base, 0, 32, sum, p);
+                        if (edge) tile_probabilities<M, CODES, true>(v[k & 1], f + 32 * k, up, c2, minus_base, lo - 32 * k, hi - 32 * k, sum, p);
+                        else tile_probabilities<M, CODES, false>(v[k & 1], f + 32 * k, up, c2, minus_base, 0, 32, sum, p);
                         ptx::tmem_st16(t_s + 16 * k, p);                // (columns whose scores have been read)
                     }
                     ptx::tmem_st_wait();

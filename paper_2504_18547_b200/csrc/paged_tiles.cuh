@@ -58,10 +58,42 @@ __device__ __forceinline__ uint32_t codes_to_16<__half>(uint32_t two) {
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(0x64806480u));        // 1152
     return r;
 }
+// Four codes of a word, in order, as fp16: one byte permute puts two of them (offset by 128) under the exponent of 1024.
+__device__ __forceinline__ uint2 codes_to_half4(uint32_t four) {
+    const uint32_t u = four ^ 0x80808080u;
+    uint2 r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r.x) : "r"(__byte_perm(u, 0x64646464u, 0x4140)), "r"(0x64806480u));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r.y) : "r"(__byte_perm(u, 0x64646464u, 0x4342)), "r"(0x64806480u));
+    return r;
+}
 // Four codes of a word, in order.
 template <typename T>
 __device__ __forceinline__ uint2 codes_to_16x4(uint32_t four) {
     return make_uint2(codes_to_16<T>(__byte_perm(four, 0u, 0x4140)), codes_to_16<T>(__byte_perm(four, 0u, 0x4342)));
+}
+
+// 2^x of a pair, -126 <= x < 128, without the special-function unit: x = n + f with n the nearest integer (the constant 1.5 * 2^23 rounds), 2^f on
+// [-1/2, 1/2] by a polynomial of degree five (weighted least squares on Chebyshev nodes until the relative error is even: 7.5e-8, 2.2e-7 with fp32
+// steps), n added to the exponent.  Eight packed operations and two integer ones take as long on the FMA pipe as the special-function unit takes for
+// two results, so a kernel that is bound by exponentials shares them between the two.
+__device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
+    const f32x2 t = f2_add(x, f2_dup(12582912.0f));
+    const f32x2 f = f2_fma(f2_add(t, f2_dup(-12582912.0f)), f2_dup(-1.0f), x);
+    f32x2 p = f2_fma(f2_dup(1.327647129e-03f), f, f2_dup(9.675540961e-03f));
+    p = f2_fma(p, f, f2_dup(5.550713092e-02f));
+    p = f2_fma(p, f, f2_dup(2.402212024e-01f));
+    p = f2_fma(p, f, f2_dup(6.931469440e-01f));
+    p = f2_fma(p, f, f2_dup(1.000000119e+00f));
+    float ta, tb;
+    f2_unpack(t, ta, tb);
+    f2_unpack(p, a, b);
+    a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23));
+    b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
+}
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 
 // A tile of 128 rows of D 16-bit channels as the tensor core wants it: lines of 64 channels, row r of line i at i * 16384 + r * 128, its 16-byte

@@ -80,6 +80,20 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pair
     grid_dependency_launch();
     const int token = blockIdx.x / P.blocks_per_token, part = blockIdx.x - token * P.blocks_per_token;
     const int half = P.rotary >> 1;
+    const int lane = threadIdx.x % LANES, c0 = lane * 8, sub = (threadIdx.x & 31) - lane;     // sub: the row's first lane in its warp
+    const int heads = P.q_heads + P.kv_heads + (P.cache_v ? P.kv_heads : 0);
+    const int end = min(heads, (part + 1) * P.heads_per_block);
+    const TI* const q0 = (const TI*)P.q + token * P.q_stride + c0;
+    const TI* const k0 = (const TI*)P.k + token * P.k_stride + c0 - P.q_heads * D;
+    const TI* const v0 = (const TI*)P.v + token * P.v_stride + c0 - (P.q_heads + P.kv_heads) * D;
+    auto load_row = [&](int h, float (&y)[8]) {
+        if (h < end) load8<TI>((h < P.q_heads ? q0 : h < P.q_heads + P.kv_heads ? k0 : v0) + h * D, y);
+    };
+    // the first row is asked for in front of the angles, every other one while its predecessor is worked on
+    int h = part * P.heads_per_block + (int)threadIdx.x / LANES;
+    float ahead[8] = {};
+    load_row(h, ahead);
+    const long long slot = P.slots ? P.slots[token] : -1;
     if ((int)threadIdx.x < half) {
         const double turns = (double)P.positions[token] * P.frequencies[threadIdx.x] * 0.15915494309189533577;   // 1 / 2 pi
         float s, c;
@@ -87,104 +101,113 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pair
         turn[threadIdx.x] = make_float2(c, s);
     }
     __syncthreads();
-    const int lane = threadIdx.x % LANES, c0 = lane * 8, sub = (threadIdx.x & 31) - lane;     // sub: the row's first lane in its warp
-    const long long slot = P.slots ? P.slots[token] : -1;
     const bool stored = slot >= 0 && slot < P.places;
     const long long page = slot >> P.page_shift;
     const int place = (int)(slot - (page << P.page_shift));
-    const int heads = P.q_heads + P.kv_heads + (P.cache_v ? P.kv_heads : 0);
-    const int end = min(heads, (part + 1) * P.heads_per_block);
+    TO* const qo = (TO*)P.q_out + token * P.q_out_stride + c0;
+    TO* const ko = (TO*)P.k_out + token * P.k_out_stride + c0;
+    const long long cache_at = page * P.page_stride + place * P.token_stride + c0, flat_at = ((page * P.cache_heads) << P.page_shift) + place;
     // every thread of a warp takes the same number of steps: the shuffles below need all of them
-    for (int h0 = part * P.heads_per_block; h0 < end; h0 += ROWS) {
-        const int h = h0 + (int)threadIdx.x / LANES;
+    for (int h0 = part * P.heads_per_block; h0 < end; h0 += ROWS, h += ROWS) {
         const bool live = h < end;
         const bool is_q = h < P.q_heads, is_v = h >= P.q_heads + P.kv_heads;
         const int hk = is_q ? h : (h - P.q_heads) - (is_v ? P.kv_heads : 0);
-        float y[8] = {};
-        if (live) {
-            const TI* row = is_q ? (const TI*)P.q + token * P.q_stride : is_v ? (const TI*)P.v + token * P.v_stride : (const TI*)P.k + token * P.k_stride;
-            load8<TI>(row + hk * D + c0, y);
-        }
-        if (norm != VITINT_NORM_NONE) {
-            float mean = 0.0f;
-            if (norm == VITINT_NORM_LAYER) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = ahead[i];
+        load_row(h + ROWS, ahead);
+        if (__any_sync(0xffffffffu, live && !is_v)) {                     // (values are neither normed nor rotated)
+            if (norm != VITINT_NORM_NONE) {
+                const float* const gain = is_q ? P.q_gain : P.k_gain;
+                const float* const offset = is_q ? P.q_offset : P.k_offset;
+                float g[8], o[8] = {};
+                if (live && !is_v) {
+                    load8<float>(gain + c0, g);
+                    if (offset) load8<float>(offset + c0, o);
+                }
+                float mean = 0.0f;
+                if (norm == VITINT_NORM_LAYER) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s += y[i];
+                    mean = row_sum<LANES>(s) * (1.0f / D);
+                }
                 float s = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += y[i];
-                mean = row_sum<LANES>(s) * (1.0f / D);
-            }
-            float s = 0.0f;
+                for (int i = 0; i < 8; ++i) { const float d = y[i] - mean; s = fmaf(d, d, s); }
+                // 1 / sqrt by the hardware's approximation and a Newton step (0 and infinity stay what the approximation makes of them)
+                const float v = row_sum<LANES>(s) * (1.0f / D) + P.eps;
+                float r = rsqrtf(v);
+                if (v > 1e-36f && v < 1e36f) r = r * fmaf(-0.5f * v * r, r, 1.5f);
+                if (live && !is_v) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { const float d = y[i] - mean; s = fmaf(d, d, s); }
-            const float r = 1.0f / sqrtf(row_sum<LANES>(s) * (1.0f / D) + P.eps);
-            if (live && !is_v) {
-                const float* gain = is_q ? P.q_gain : P.k_gain;
-                const float* offset = is_q ? P.q_offset : P.k_offset;
-                float g[8], o[8] = {};
-                load8<float>(gain + c0, g);
-                if (offset) load8<float>(offset + c0, o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = fmaf((y[i] - mean) * r, g[i], o[i]);
-            }
-        }
-        if (half) {
-            const bool turned = !is_v && c0 < P.rotary;
-            if (pairs) {
-                if (turned) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 t = turn[(c0 >> 1) + i];
-                        const float a = y[2 * i], b = y[2 * i + 1];
-                        y[2 * i] = fmaf(a, t.x, -b * t.y);
-                        y[2 * i + 1] = fmaf(b, t.x, a * t.y);
-                    }
+                    for (int i = 0; i < 8; ++i) y[i] = fmaf((y[i] - mean) * r, g[i], o[i]);
                 }
-            } else {
-                const bool low = c0 < half;
-                const int from = sub + (lane + (low ? half / 8 : LANES - half / 8)) % LANES;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float other = __shfl_sync(0xffffffffu, y[i], from);
+            }
+            if (half) {
+                const bool turned = !is_v && c0 < P.rotary;
+                if (pairs) {
                     if (turned) {
-                        const float2 t = turn[(low ? c0 : c0 - half) + i];
-                        y[i] = fmaf(y[i], t.x, low ? -other * t.y : other * t.y);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 t = turn[(c0 >> 1) + i];
+                            const float a = y[2 * i], b = y[2 * i + 1];
+                            y[2 * i] = fmaf(a, t.x, -b * t.y);
+                            y[2 * i + 1] = fmaf(b, t.x, a * t.y);
+                        }
+                    }
+                } else {
+                    const bool low = c0 < half;
+                    const int from = sub + (lane + (low ? half / 8 : LANES - half / 8)) % LANES;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float other = __shfl_sync(0xffffffffu, y[i], from);
+                        if (turned) {
+                            const float2 t = turn[(low ? c0 : c0 - half) + i];
+                            y[i] = fmaf(y[i], t.x, low ? -other * t.y : other * t.y);
+                        }
                     }
                 }
             }
         }
-        float step = 0.0f, scale = 0.0f;
-        if (CODES) {                                                     // (queries take part in the shuffles)
+        float step = 0.0f;
+        if (CODES && __any_sync(0xffffffffu, live && !is_q)) {
             float m = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
             step = __fdiv_rn(row_max<LANES>(m), 127.0f);
-            scale = step;
         }
         if (!live) continue;
         if (is_q) {
-            store8<TO>((TO*)P.q_out + token * P.q_out_stride + hk * D + c0, y);
+            store8<TO>(qo + hk * D, y);
             continue;
         }
-        if (!is_v && P.k_out) store8<TO>((TO*)P.k_out + token * P.k_out_stride + hk * D + c0, y);
+        if (!is_v && P.k_out) store8<TO>(ko + hk * D, y);
         if (!stored) continue;
-        const long long at = page * P.page_stride + hk * P.head_stride + place * P.token_stride + c0;
-        const long long flat = ((page * P.cache_heads + hk) << P.page_shift) + place;
+        const long long at = cache_at + hk * P.head_stride;
         void* const base = is_v ? P.cache_v : P.cache_k;
         if (CODES) {
             uint32_t w[2] = {0u, 0u};
-            if (scale > 0.0f) {
+            // the quotient by the step's reciprocal; at most 127 (1 + 2^-22), which needs no clamp, unless the step is denormal
+            if (step >= 1e-37f) {
+                const float r = __frcp_rn(step);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int code = (int)fminf(fmaxf(rintf(__fdiv_rn(y[i], scale)), -127.0f), 127.0f);
-                    w[i >> 2] |= (uint32_t)(code & 255) << (8 * (i & 3));
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) u[k] = __float_as_uint(fmaf(y[4 * i + k], r, 12582912.0f));       // rounded to an integer in the low bits
+                    w[i] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
                 }
+            } else if (step > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i >> 2] |= (round_clamp_bits(__fdiv_rn(y[i], step), -127.0f, 127.0f) & 255u) << (8 * (i & 3));
             }
             *reinterpret_cast<uint2*>((int8_t*)base + at) = make_uint2(w[0], w[1]);
-            if (lane == 0) (is_v ? P.v_steps : P.k_steps)[flat] = step;
+            if (lane == 0) (is_v ? P.v_steps : P.k_steps)[flat_at + ((long long)hk << P.page_shift)] = step;
         } else {
             store8<TO>((TO*)base + at, y);
         }
-        if (lane == 0 && !is_v && P.weights) P.weights[flat] = 0.0f;
+        if (lane == 0 && !is_v && P.weights) P.weights[flat_at + ((long long)hk << P.page_shift)] = 0.0f;
     }
 }
 

@@ -88,11 +88,12 @@ def visible(length, new, causal, window):
 def attention64(q, cache, table, lengths, starts, scale, causal, window):
     """(out, lse, tolerance of out, tolerance of lse, rows that belong to a sequence) in 64 bits.
 
-    A kernel that keeps scores, maxima and sums in fp32, rounds each probability (times a step) to the type T before the second
+    A kernel that keeps scores, maxima and sums in fp32, rounds each probability (times a step) to the type T or more finely before the second
     contraction and the output once is off by at most
       eps/2 |o|                          the output's rounding (eps/2 is half a step of T),
       eps/2 sum p |v|                    the probabilities' rounding (normal ones),
-      2^-25 L max|v|                     fp16 only: probabilities below the normal range (relative to a maximum of 1 or more),
+      2^-25 L max|v|                     fp16 and codes: probabilities (times steps) below fp16's normal range, relative to a
+                                         maximum of 1 or more (times the power of two of the largest step),
       (2 ds + 2^-19) sum p |v|           ds: error of a score, (d + 4) 2^-24 scale sum |q||k| for d products and their sum, the step and
                                          the scale, and 2^-24 |s| each for the maximum's subtraction; the sum of exponentials has it
                                          too; 2^-19 covers ex2's 2^-22, the sums' and rescalings' roundings.
@@ -121,7 +122,7 @@ def attention64(q, cache, table, lengths, starts, scale, causal, window):
             out[first:first + new, h], lse[first:first + new, h] = o, z
             pv = p @ v.abs()
             tol[first:first + new, h] = half * o.abs() + (half * 1.01 + 2 * ds[:, None] + 2.0 ** -19) * pv
-            if q.dtype == torch.float16:
+            if q.dtype == torch.float16 or cache.k.dtype == torch.int8:
                 tol[first:first + new, h] += 2.0 ** -25 * length * v.abs().max()
             lse_tol[first:first + new, h] = ds + 2.0 ** -19 + 2.0 ** -22 * z.abs().masked_fill(z == -math.inf, 0)
     return out, lse, tol, lse_tol, mine
