@@ -495,7 +495,7 @@ typedef struct {
  *     reduction to one turn in fp64: the pair (y1, y2) becomes (y1 cos a_i - y2 sin a_i, y2 cos a_i + y1 sin a_i).  pairs == 0:
  *     channels i and i + rotary/2; pairs == 1: channels 2i and 2i + 1.  Values (v) are neither normed nor rotated.
  *   Results are rounded once: to out_type in q_out and k_out, to the cache's type in the cache; codes take the step
- *   max|y| / 127 of their head row and q = rint(y / step), the quotient within 2 ulp (a row of zeros has step 0 and codes 0).
+ *   max|y| / 127 of their head row (within an ulp) and q = rint(y / step), the quotient within 2 ulp (a row of zeros has step 0 and codes 0).
  *   q: [tokens, q_heads*head_dim] of in_type (VITINT_F32, BF16, F16), rows q_stride elements apart; k, v: [tokens, kv_heads*head_dim]
  *     with k_stride, v_stride.  Pointers and strides in bytes are multiples of 16.  q may be NULL with q_heads 0.
  *   gains, offsets: device fp32 [head_dim] (offsets for LAYER only, NULL otherwise; gains NULL for NONE).

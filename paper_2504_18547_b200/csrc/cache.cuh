@@ -151,12 +151,16 @@ __device__ __forceinline__ Sequence sequence_of(const SequenceView& s, int b) {
     return sequence_of(s, b, unused);
 }
 
-// Page of a sequence's token; one outside the cache is reported and given as `pages` (nothing lies there: the TMA fills in zeros).
-__device__ __forceinline__ int page_of(const SequenceView& s, int b, int token) {
-    const int p = s.page_table[(long long)b * s.table_stride + (token >> s.page_shift)];
-    if ((unsigned)p < (unsigned)s.pages) return p;
+// Page table entry of a sequence's token.  An entry outside the cache is reported where it is used and counts as `pages` (nothing lies there: the
+// TMA fills in zeros).  The two are apart so that a kernel can ask for entries ahead of their use: a check waits for what it checks.
+__device__ __forceinline__ int page_entry(const SequenceView& s, int b, int token) {
+    return s.page_table[(long long)b * s.table_stride + (token >> s.page_shift)];
+}
+__device__ __forceinline__ int checked_page(const SequenceView& s, int entry) {
+    if ((unsigned)entry < (unsigned)s.pages) return entry;
     report_bad_data();
     return s.pages;
 }
+__device__ __forceinline__ int page_of(const SequenceView& s, int b, int token) { return checked_page(s, page_entry(s, b, token)); }
 
 }  // namespace vitint

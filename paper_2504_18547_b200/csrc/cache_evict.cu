@@ -5,7 +5,7 @@
 // summed over the cluster, then the digit in which the count is reached), and then one pass in token order that writes the indices above
 // it and the first ones equal to it.  The weights are read once and stay in shared memory.  Bound by latency: three histograms and their sums
 // follow one another; clusters are as large as the GPU has room for and a block has 2048 tokens left.
-// 65,536 tokens x 8 heads: 120 -> EVICT_LONG us against one block a head that reads its weights anew for every pass.
+// 65,536 tokens x 8 heads: 120 -> 27 us against one block a head that reads its weights anew for every pass.
 // Move: bound by HBM.  A warp takes 32 kept tokens: its lanes look up where they lie and go, then all of them copy row after row, sixteen bytes a
 // lane, eight rows under way.
 #include "cache.cuh"
@@ -63,10 +63,19 @@ __device__ __forceinline__ uint32_t cluster_rank() { uint32_t v; asm("mov.u32 %0
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
-__device__ __forceinline__ uint32_t remote_word(const uint32_t* mine, uint32_t rank) {         // the same variable of another block
-    uint32_t addr = ptx::smem_addr(mine), at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at));                     // (ordered by the barriers around)
+__device__ __forceinline__ uint32_t remote_address(const void* mine, uint32_t rank) {           // of the same variable of another block
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(ptx::smem_addr(mine)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ uint32_t remote_word(const uint32_t* mine, uint32_t rank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote_address(mine, rank)));      // (ordered by the barriers around)
+    return v;
+}
+__device__ __forceinline__ uint4 remote_quad(const uint4* mine, uint32_t rank) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote_address(mine, rank)));
     return v;
 }
 
@@ -75,7 +84,7 @@ __device__ __forceinline__ uint32_t remote_word(const uint32_t* mine, uint32_t r
 __global__ void __launch_bounds__(EV_THREADS)
 evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
     extern __shared__ uint32_t ev_keys[];
-    __shared__ uint32_t bins[2][EV_BINS];
+    __shared__ __align__(16) uint32_t bins[2][EV_BINS];                // the largest digit first
     __shared__ unsigned long long warp_sums[32];
     __shared__ uint32_t found[2];                                      // the digit, and how many are still wanted inside it
     __shared__ uint32_t larger_of[33], equal_of[33];                   // counts of the block's warps, then of the block
@@ -108,10 +117,26 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
         return weight_key(p < P.seq.pages ? P.weights[(((long long)p * P.kv_heads + h) << shift) + ((begin + i) & mask)] : 0.0f);
     };
     const bool in_shared = n <= held;
+    auto barrier = [&] {
+        if (blocks > 1) cluster_barrier();
+        else __syncthreads();
+    };
     auto key_of = [&](int i) { return in_shared ? ev_keys[i] : read_key(i); };
     if (in_shared) {
-#pragma unroll 8
-        for (int i = t; i < n; i += EV_THREADS) ev_keys[i] = read_key(i);
+        for (int i0 = t; i0 < n; i0 += 8 * EV_THREADS) {               // eight tokens of a thread under way
+            int page[8];
+            float w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) page[k] = i0 + k * EV_THREADS < n ? page_entry(P.seq, b, begin + i0 + k * EV_THREADS) : 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * EV_THREADS, p = i < n ? checked_page(P.seq, page[k]) : P.seq.pages;
+                w[k] = p < P.seq.pages ? P.weights[(((long long)p * P.kv_heads + h) << shift) + ((begin + i) & mask)] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k * EV_THREADS < n) ev_keys[i0 + k * EV_THREADS] = weight_key(w[k]);
+        }
     }
     __syncthreads();
     uint32_t prefix = 0, known = 0;                                    // digits found so far, and their bits
@@ -121,32 +146,42 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
         const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 1023u : 2047u;
         uint32_t* const mine = bins[pass & 1];
-        for (int i = t; i < n; i += EV_THREADS) {
-            const uint32_t k = key_of(i);
-            // equal digits of a warp are counted together: many tokens have the same weight (none), and their additions would queue up
-            if ((k & known) == prefix) {
-                const uint32_t digit = (k >> low) & digits, same = __match_any_sync(__activemask(), digit);
-                if (lane == __ffs(same) - 1) atomicAdd(&mine[digit], (uint32_t)__popc(same));
+        for (int i = t; i - lane < n; i += EV_THREADS) {
+            const uint32_t k = i < n ? key_of(i) : 0u, digit = digits - ((k >> low) & digits);
+            const bool counted = i < n && (k & known) == prefix;
+            // (a warp whose tokens all have one weight, none as a rule, counts them together: their additions would queue up)
+            const bool leads = digit == __shfl_sync(0xffffffffu, digit, 0);
+            if (__all_sync(0xffffffffu, counted && leads)) {
+                if (lane == 0) atomicAdd(&mine[digit], 32u);
+            } else if (counted) {
+                atomicAdd(&mine[digit], 1u);
             }
         }
-        cluster_barrier();
+        barrier();
         // (the other histogram was last read in front of this barrier)
         for (int i = t; i < EV_BINS; i += EV_THREADS) bins[(pass + 1) & 1][i] = 0u;
-        // digits from the largest down: thread t has EV_BINS-1-2t and EV_BINS-2-2t, over all blocks
-        const uint32_t d0 = EV_BINS - 1 - 2 * t, d1 = d0 - 1;
-        uint32_t n0 = mine[d0], n1 = mine[d1];
-        if (blocks > 1) {
+        // four digits a thread, over all blocks
+        uint4 q = make_uint4(0u, 0u, 0u, 0u);
+        if (t < EV_BINS / 4) {
+            const uint4* const at = reinterpret_cast<const uint4*>(mine) + t;
+            q = *at;
+            if (blocks > 1) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r)                                 // (all of them under way at once)
-                if (r < blocks && r != rank) {
-                    n0 += remote_word(&mine[d0], r);
-                    n1 += remote_word(&mine[d1], r);
-                }
+                for (int r = 0; r < 8; ++r)                             // (all of them under way at once)
+                    if (r < blocks && r != rank) {
+                        const uint4 o = remote_quad(at, r);
+                        q.x += o.x; q.y += o.y; q.z += o.z; q.w += o.w;
+                    }
+            }
         }
         unsigned long long total;
-        const uint32_t above = (uint32_t)block_scan(n0 + n1, warp_sums, total);
-        if (above < want && want <= above + n0) { found[0] = d0; found[1] = want - above; }
-        else if (above + n0 < want && want <= above + n0 + n1) { found[0] = d1; found[1] = want - above - n0; }
+        uint32_t above = (uint32_t)block_scan(q.x + q.y + q.z + q.w, warp_sums, total);
+        const uint32_t count_of[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (above < want && want <= above + count_of[k]) { found[0] = digits - (uint32_t)(4 * t + k); found[1] = want - above; }
+            above += count_of[k];
+        }
         __syncthreads();
         prefix |= found[0] << low;
         known |= digits << low;
@@ -178,7 +213,7 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
         equal_of[lane] = pe - e;
         if (lane == 0) { larger_of[32] = sa; equal_of[32] = se; }
     }
-    cluster_barrier();
+    barrier();
     uint32_t ahead_larger = larger_of[warp], ahead_equal = equal_of[warp];
     for (int r = 0; r < rank; ++r) {
         ahead_larger += remote_word(&larger_of[32], r);
@@ -194,7 +229,7 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
         ahead_larger += __popc(a);
         ahead_equal += __popc(e);
     }
-    cluster_barrier();                                                 // the others have read this block's counts
+    if (blocks > 1) cluster_barrier();                                 // the others have read this block's counts
 }
 
 struct MoveParams {
@@ -276,7 +311,9 @@ inline cudaError_t launch_select(const EvictParams& E, int sequences, int cluste
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(E.kv_heads * cluster), (unsigned)sequences);
     cfg.blockDim = dim3(EV_THREADS);
+    // (blocks of a cluster do not share an SM, which two of them may when they are placed early: so much that only one fits)
     cfg.dynamicSmemBytes = (size_t)held * 4;
+    if (cluster > 1 && cfg.dynamicSmemBytes < 116 * 1024) cfg.dynamicSmemBytes = 116 * 1024;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -3,11 +3,14 @@
 // With keys as the rows of the product S^T = K Q^T (tcgen05, 128 keys x up to 128 query rows) a thread has a key: it sums over the columns that
 // tensor memory gives it, and nothing crosses threads.  The rows' logarithms of sums come from the attention call, so one pass does.
 //
-// For prompts it is bound by the exponentials (16 a clock and SM: 1024 cycles for 128 x 128 scores, whose product takes 512; a part of them goes
-// through the FMA pipe), for single tokens by reading the keys.  Two tiles of keys stay in shared memory while the query tiles that see
-// them stream past (one tile would have 32 KB of queries come from L2 for every 128 x 128 scores, which alone takes 1900 cycles); a group of four
-// warps has the scores of one of them, in two buffers each.  Work is shared out evenly as for the attention (paged_plan.cuh), with keys and queries
-// in each other's places; a run of keys whose queries are split between CTAs is summed by a second kernel in the CTAs' order.
+// For prompts it is bound by shared memory: the product of 128 x 128 scores reads 64 KB of operands, which is what shared memory delivers in its
+// 512 cycles, and every thread loads the rows' logarithms beside it (1023 tokens x 32 heads over 12,287 cached codes: 151 us, 660 TFLOP/s; without
+// these loads 121, with a quarter of the products 140; loading them once for two keys of a thread costs registers: 167).  The exponentials, 16 a clock
+// and SM, take 1024 cycles of the special-function unit; a part of them goes through the FMA pipe (all through the unit: 164 us).  For single tokens it
+// is bound by reading the keys.  Two tiles of keys stay in shared memory while the query tiles that see them stream past (one would have 32 KB
+// of queries come from L2 for every 128 x 128 scores); a group of four warps has the scores of one of them, in two buffers each.  Work is shared out
+// evenly as for the attention (paged_plan.cuh), with keys and queries in each other's places; a run of keys whose queries are split between CTAs is
+// summed by a second kernel in the CTAs' order.
 #include "paged_tiles.cuh"
 
 namespace vitint {
@@ -119,7 +122,6 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const Stretch r = plan_stretch<Runs>(P.plan, blockIdx.x, gridDim.x, bad);
         if (lane == 0) {
             shared_stretch = r;
-            P.notes[blockIdx.x] = join_note(r, blockIdx.x);
             if (bad && blockIdx.x == 0) report_bad_data();
         }
     }
@@ -128,6 +130,8 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     ptx::tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     StretchWalk<Runs> w;
+    // (by a thread that waits for its first tile anyway)
+    if (threadIdx.x == 32) P.notes[blockIdx.x] = join_note(P.plan, shared_stretch, blockIdx.x);
     w.begin(P.plan, shared_stretch);
     bool ok = true;
     auto halves = [](const StretchWalk<Runs>& at) { return at.s.length - at.p * CW_KEYS > CW_HALF ? 2 : 1; };
@@ -140,16 +144,14 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int k_ring = CODES ? P.raw_stages : P.k_stages;
         const uint32_t k_base = smem + (CODES ? P.off_raw : P.off_k), k_slot = CODES ? RAW_SLOT : K_SLOT;
         // lane r looks up the item's r-th run of page rows, an item ahead
-        auto page_at = [&](const StretchWalk<Runs>& at) {
-            const int key = at.p * CW_KEYS + lane * P.page_rows;
-            return at.more() && lane < 2 * copies && key < at.s.length ? page_of(P.plan.seq, at.b, key) : -1;
-        };
+        auto key_at = [&](const StretchWalk<Runs>& at) { return at.p * CW_KEYS + lane * P.page_rows; };
+        auto copied = [&](const StretchWalk<Runs>& at) { return at.more() && lane < 2 * copies && key_at(at) < at.s.length; };
         StretchWalk<Runs> next = w;
-        int next_page = page_at(next);
+        int entry = copied(w) ? page_entry(P.plan.seq, w.b, key_at(w)) : 0;
         for (; ok && w.more(); w = next) {
-            const int page = next_page;
+            const int page = copied(w) ? checked_page(P.plan.seq, entry) : -1;
             next.next(P.plan);
-            next_page = page_at(next);
+            if (copied(next)) entry = page_entry(P.plan.seq, next.b, key_at(next));
             for (int x = 0; x < halves(w); ++x) {
                 const bool mine = page >= 0 && lane / copies == x;
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, mine));
@@ -273,18 +275,18 @@ cache_weigh_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const float before = w.whole() && inside && P.in ? P.in[at] : 0.0f;
             const f32x2 c2 = f2_dup(P.c * step);
             f32x2 acc[2] = {f2_dup(0.0f), f2_dup(0.0f)};
+            const int row_token = row / P.plan.group, row_head = w.h * P.plan.group + row - row_token * P.plan.group;
             auto rows_of = [&](int t) { return min(P.plan.tile_tokens, w.s.queries - (w.first + t) * P.plan.tile_tokens) * P.plan.group; };
             auto lse_of = [&](int t) {                                 // of this thread's row of tile t
-                if (t >= w.end || row >= rows_of(t)) return -INFINITY;
-                const int i = row / P.plan.group;
-                const float l = P.lse[(long long)(w.s.first + (w.first + t) * P.plan.tile_tokens + i) * P.q_heads + w.h * P.plan.group + row - i * P.plan.group];
-                return l == -INFINITY ? -INFINITY : l * -1.4426950408889634f;      // a row that saw nothing gives nothing
+                if (t >= w.end || row >= rows_of(t)) return INFINITY;
+                return P.lse[(long long)(w.s.first + (w.first + t) * P.plan.tile_tokens + row_token) * P.q_heads + row_head];
             };
             float next = lse_of(w.tile);
             for (int t = w.tile; t < w.end; ++t, ++n_s) {
                 const uint32_t buffer = n_s & 1u;
                 float* const l = minus_lse[x][buffer];
-                if (row < (int)COLS) l[row] = next;
+                // (the value asked for a tile ahead; a row that saw nothing gives nothing)
+                if (row < (int)COLS) l[row] = next == -INFINITY ? -INFINITY : next * -1.4426950408889634f;
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + x) : "memory");
                 next = lse_of(t + 1);
                 ok = ok && mbar_wait_warp(ptx::smem_addr(&B.s_full[x][buffer]), (n_s >> 1) & 1u, abort_ptr);
@@ -342,7 +344,7 @@ cache_weigh_join_kernel(const __grid_constant__ WeighParams P) {
     grid_dependency_launch();
     const JoinNote n = P.notes[blockIdx.x + 1];
     if (n.last_cta < 0) return;
-    const Sequence s = sequence_of(P.plan.seq, n.b);
+    const Sequence s{n.length, n.first, n.queries};
     const int key = n.p * CW_KEYS + (int)threadIdx.x;
     if (key >= s.length) return;
     const int page = page_of(P.plan.seq, n.b, key);

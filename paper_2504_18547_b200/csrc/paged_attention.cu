@@ -182,12 +182,13 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const Stretch r = plan_stretch<Runs>(P.plan, blockIdx.x, gridDim.x, bad);
         if (lane == 0) {
             *shared_stretch = r;
-            P.notes[blockIdx.x] = join_note(r, blockIdx.x);
             if (bad && blockIdx.x == 0) report_bad_data();
         }
     }
     __syncthreads();
     StretchWalk<Runs> w;
+    // (by a thread that waits for its first tile anyway)
+    if (threadIdx.x == 32) P.notes[blockIdx.x] = join_note(P.plan, *shared_stretch, blockIdx.x);
     w.begin(P.plan, *shared_stretch);
     bool ok = true;
     int stage = 0;
@@ -202,16 +203,16 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         const int page_mask = (1 << P.plan.seq.page_shift) - 1;
         int issued = 0;
         for (; ok && w.more(); w.next(P.plan)) {
-            auto page_at = [&](int t) {
-                const int key = w.first + t * KT + lane * P.page_rows;
-                return lane < copies && t < w.end && key < w.s.length ? page_of(P.plan.seq, w.b, key) : -1;
-            };
-            int next = page_at(w.tile);
+            auto key_at = [&](int t) { return w.first + t * KT + lane * P.page_rows; };
+            auto copied = [&](int t) { return lane < copies && t < w.end && key_at(t) < w.s.length; };
+            int next = copied(w.tile) ? page_entry(P.plan.seq, w.b, key_at(w.tile)) : 0;
             for (int t = w.tile; t < w.end; ++t) {
-                const int key = w.first + t * KT + lane * P.page_rows, page = next;
-                const bool mine = page >= 0, inside = mine && page < P.plan.seq.pages;
+                const int key = key_at(t);
+                const bool mine = copied(t);
+                const int page = mine ? checked_page(P.plan.seq, next) : 0;
+                const bool inside = mine && page < P.plan.seq.pages;
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, mine)), n_steps = __popc(__ballot_sync(0xffffffffu, inside));
-                next = page_at(t + 1);
+                if (copied(t + 1)) next = page_entry(P.plan.seq, w.b, key_at(t + 1));
                 ok = mbar_wait_warp(bars + 8 * (STAGES + stage), phase ^ 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t full = bars + 8 * stage;
@@ -607,22 +608,39 @@ paged_rows_join_kernel(const __grid_constant__ RowsParams P) {
         for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; }
 #pragma unroll
     for (int e = 0; e < 4 * NQ; ++e) o[e] = 0.0f;
-#pragma unroll 4
-    for (int cta = note.first_cta; cta <= note.last_cta; ++cta) {
-        const float* const at = P.partial + (2ll * cta + (cta == note.first_cta ? 1 : 0)) * S::PART;
+    constexpr int DEEP = 8 / NQ;                                       // parts whose loads are under way at once
+    for (int cta0 = note.first_cta; cta0 <= note.last_cta; cta0 += DEEP) {
+        float v[DEEP][4 * NQ], pm[DEEP][NQ][2], pl[DEEP][NQ][2];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
+        for (int i = 0; i < DEEP; ++i) {
+            const int cta = cta0 + i;
+            const bool there = cta <= note.last_cta;
+            const float* const at = P.partial + (2ll * cta + (cta == note.first_cta ? 1 : 0)) * S::PART;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float top, mine, theirs;
-                join_scales(m[n][e], at[S::NREG * 32 + 8 * n + 2 * c + e], top, mine, theirs);
-                m[n][e] = top;
-                l[n][e] = l[n][e] * mine + at[S::NREG * 32 + 8 * (NQ + n) + 2 * c + e] * theirs;
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) o[4 * n + 2 * r + e] = o[4 * n + 2 * r + e] * mine + at[(mt * 4 * NQ + 4 * n + 2 * r + e) * 32 + lane] * theirs;
-            }
+                for (int e = 0; e < 2; ++e) {
+                    pm[i][n][e] = there ? at[S::NREG * 32 + 8 * n + 2 * c + e] : -INFINITY;
+                    pl[i][n][e] = there ? at[S::NREG * 32 + 8 * (NQ + n) + 2 * c + e] : 0.0f;
+                }
+#pragma unroll
+            for (int e = 0; e < 4 * NQ; ++e) v[i][e] = there ? at[(mt * 4 * NQ + e) * 32 + lane] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top, mine, theirs;
+                    join_scales(m[n][e], pm[i][n][e], top, mine, theirs);
+                    m[n][e] = top;
+                    l[n][e] = l[n][e] * mine + pl[i][n][e] * theirs;
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) o[4 * n + 2 * r + e] = o[4 * n + 2 * r + e] * mine + v[i][4 * n + 2 * r + e] * theirs;
+                }
     }
-    const Sequence s = sequence_of(P.plan.seq, note.b);
+    const Sequence s{note.length, note.first, note.queries};
     float inv[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)

@@ -25,10 +25,11 @@ struct TilesShape {
     static constexpr int LINES = D / 64;
     static constexpr int OPERAND = LINES * 16384;                       // a tile of 128 rows as an operand
     static constexpr int RAW = PT_KEYS * D;                             // ... of codes as they come
-    static constexpr int SLOTS = CODES ? (D == 128 ? 4 : 8) : (D == 128 ? 5 : 10);
+    static constexpr int Q_BUFFERS = D == 64 ? 2 : 1;                   // the next item's queries arrive beside this one's where there is room
+    static constexpr int SLOTS = CODES ? (D == 128 ? 4 : 6) : (D == 128 ? 5 : 8);
     static constexpr int RAW_SLOTS = CODES ? (D == 128 ? 2 : 4) : 0;
     static constexpr int THREADS = (CODES ? 14 : 10) * 32;
-    static constexpr int STEPS = 2 * OPERAND + SLOTS * OPERAND + RAW_SLOTS * RAW;       // offsets: codes' steps, barriers
+    static constexpr int STEPS = (2 * Q_BUFFERS + SLOTS) * OPERAND + RAW_SLOTS * RAW;       // offsets: codes' steps, barriers
     static constexpr int TAIL = STEPS + (CODES ? PT_STEP_SLOTS * 2 * PT_KEYS * 4 : 0);
     static constexpr int SMEM = TAIL + 512;
     static constexpr int PART = 2 * (D + 2) * 128;                      // floats of a partial result: [half][output columns, maximum, sum][row]
@@ -48,7 +49,7 @@ struct TilesParams {
 };
 
 struct TilesBars {
-    uint64_t q_full, q_empty, full[PT_MAX_SLOTS], empty[PT_MAX_SLOTS], raw_full[4], raw_empty[4], steps_full[PT_STEP_SLOTS], steps_empty[PT_STEP_SLOTS],
+    uint64_t q_full[2], q_empty[2], full[PT_MAX_SLOTS], empty[PT_MAX_SLOTS], raw_full[4], raw_empty[4], steps_full[PT_STEP_SLOTS], steps_empty[PT_STEP_SLOTS],
         s_full[2], p_full[2], pv_done[2], drained;
 };
 
@@ -89,9 +90,9 @@ __device__ __forceinline__ Half half_of(const TilesParams& P, const StretchWalk<
     return h;
 }
 
-// Scores of 32 keys in units of log2 (not yet c-scaled where there are no codes): the maximum with what was there.
-template <bool CODES, bool MASKED>
-__device__ __forceinline__ void tile_max(const uint32_t (&v)[32], const float* steps, int low, int high, float (&top)[4]) {
+// Scores of 32 keys (those of codes times the keys' steps): the maximum with what was there.
+template <bool CODES, bool EDGE>
+__device__ __forceinline__ void tile_max(const uint32_t (&v)[32], const float* steps, uint32_t seen, float (&top)[4]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 4) {
         float4 f;
@@ -100,15 +101,16 @@ __device__ __forceinline__ void tile_max(const uint32_t (&v)[32], const float* s
         for (int k = 0; k < 4; ++k) {
             float s = __uint_as_float(v[i + k]);
             if (CODES) s *= k == 0 ? f.x : k == 1 ? f.y : k == 2 ? f.z : f.w;
-            if (MASKED) s = i + k >= low && i + k < high ? s : -INFINITY;
+            if (EDGE && !(seen & (1u << (i + k)))) s = -INFINITY;
             top[k] = fmaxf(top[k], s);
         }
     }
 }
 
-// Probabilities of 32 keys: 2^(s c - base), their sum, and 16 bits of each (times the value's step) for the second product.
-template <typename T, bool CODES, bool MASKED>
-__device__ __forceinline__ void tile_probabilities(const uint32_t (&v)[32], const float* steps, float up, f32x2 c2, f32x2 minus_base, int low, int high, f32x2 (&sum)[2],
+// Probabilities of 32 keys: 2^(s c - base), their sum, and 16 bits of each (times the value's step) for the second product.  EDGE: some keys are
+// hidden; what their scores and steps are, behind the length anything, does not matter.
+template <typename T, bool CODES, bool EDGE>
+__device__ __forceinline__ void tile_probabilities(const uint32_t (&v)[32], const float* steps, uint32_t seen, float up, f32x2 c2, f32x2 minus_base, f32x2 (&sum)[2],
                                                    uint32_t (&out)[16]) {
 #pragma unroll
     for (int i = 0; i < 32; i += 4) {
@@ -124,13 +126,13 @@ __device__ __forceinline__ void tile_probabilities(const uint32_t (&v)[32], cons
             s = f2_fma(s, c2, minus_base);
             float a, b;
             f2_unpack(s, a, b);
-            const bool ha = MASKED && !(i + 2 * k >= low && i + 2 * k < high), hb = MASKED && !(i + 2 * k + 1 >= low && i + 2 * k + 1 < high);
-            a = ha ? 0.0f : exp2_approx(a);
-            b = hb ? 0.0f : exp2_approx(b);
+            const bool seen_a = !EDGE || (seen & (1u << (i + 2 * k))), seen_b = !EDGE || (seen & (2u << (i + 2 * k)));
+            a = seen_a ? exp2_approx(a) : 0.0f;
+            b = seen_b ? exp2_approx(b) : 0.0f;
             sum[k] = f2_add(sum[k], f2_pack(a, b));
             if (CODES) {
-                a = ha ? 0.0f : a * ((k ? vf.z : vf.x) * up);
-                b = hb ? 0.0f : b * ((k ? vf.w : vf.y) * up);
+                a = seen_a ? a * ((k ? vf.z : vf.x) * up) : 0.0f;
+                b = seen_b ? b * ((k ? vf.w : vf.y) * up) : 0.0f;
             }
             out[(i >> 1) + k] = pack16<T>(a, b);
         }
@@ -157,14 +159,14 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     volatile int* const abort_ptr = &tail.abort_flag;
     const uint32_t smem = ptx::smem_addr(pt_smem);
     uint8_t* const gen = pt_smem;
-    const uint32_t ring = smem + 2 * S::OPERAND, raw_ring = ring + S::SLOTS * S::OPERAND;
+    const uint32_t ring = smem + 2 * S::Q_BUFFERS * S::OPERAND, raw_ring = ring + S::SLOTS * S::OPERAND;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         tail.abort_flag = 0;
         auto init = [&](uint64_t* b, int n, int count) { for (int i = 0; i < n; ++i) ptx::mbar_init(ptx::smem_addr(b + i), count); };
-        init(&B.q_full, 1, 1);
-        init(&B.q_empty, 1, 1);
+        init(B.q_full, 2, 1);
+        init(B.q_empty, 2, 1);
         init(B.full, PT_MAX_SLOTS, CODES ? 4 : 1);
         init(B.empty, PT_MAX_SLOTS, 1);
         init(B.raw_full, 4, 1);
@@ -190,7 +192,6 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const Stretch r = plan_stretch<Runs>(P.plan, blockIdx.x, gridDim.x, bad);
         if (lane == 0) {
             tail.stretch = r;
-            P.notes[blockIdx.x] = join_note(r, blockIdx.x);
             if (bad && blockIdx.x == 0) report_bad_data();
         }
     }
@@ -199,6 +200,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     ptx::tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tail.tmem_slot, 0);
     StretchWalk<Runs> w;
+    // (by a thread that waits for its first tile anyway)
+    if (threadIdx.x == 32) P.notes[blockIdx.x] = join_note(P.plan, tail.stretch, blockIdx.x);
     w.begin(P.plan, tail.stretch);
     bool ok = true;
 
@@ -210,29 +213,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         constexpr int RING = CODES ? S::RAW_SLOTS : S::SLOTS;
         uint64_t *const full = CODES ? B.raw_full : B.full, *const empty = CODES ? B.raw_empty : B.empty;
         for (; ok && w.more(); w.next(P.plan)) {
-            ok = mbar_wait_warp(ptx::smem_addr(&B.q_empty), (uint32_t)(items & 1) ^ 1u, abort_ptr);
-            if (!ok) break;
-            ++items;
-            if (ptx::elect_one()) {
-                const uint32_t bar = ptx::smem_addr(&B.q_full);
-                const int second = w.p * P.plan.tile_tokens + P.half_tokens < w.s.queries ? 2 : 1;
-                ptx::mbar_arrive_expect_tx(bar, second * LINES * P.box_rows * 128);
-                for (int x = 0; x < second; ++x)
-                    for (int i = 0; i < LINES; ++i)
-                        ptx::tma_load_4d(smem + x * S::OPERAND + i * 16384, &map_q, bar, 0, w.h * P.plan.group,
-                                         w.s.first + w.p * P.plan.tile_tokens + x * P.half_tokens, i);
-            }
-            __syncwarp();
-            auto page_at = [&](int t) {
-                const int key = w.first + t * PT_KEYS + lane * P.page_rows;
-                return lane < copies && t < w.end && key < w.s.length ? page_of(P.plan.seq, w.b, key) : -1;
-            };
-            int page = page_at(w.tile);
+            auto key_at = [&](int t) { return w.first + t * PT_KEYS + lane * P.page_rows; };
+            auto copied = [&](int t) { return lane < copies && t < w.end && key_at(t) < w.s.length; };
+            int next = copied(w.tile) ? page_entry(P.plan.seq, w.b, key_at(w.tile)) : 0;
             for (int t = w.tile; ok && t < w.end; ++t) {
-                const int key = w.first + t * PT_KEYS + lane * P.page_rows, here = page;
-                const bool mine = here >= 0, inside = mine && here < P.plan.seq.pages;
+                const int key = key_at(t);
+                const bool mine = copied(t);
+                const int here = mine ? checked_page(P.plan.seq, next) : 0;
+                const bool inside = mine && here < P.plan.seq.pages;
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, mine));
-                page = page_at(t + 1);
+                if (copied(t + 1)) next = page_entry(P.plan.seq, w.b, key_at(t + 1));
                 if (CODES) {
                     const uint32_t n_steps = __popc(__ballot_sync(0xffffffffu, inside));
                     ok = mbar_wait_warp(ptx::smem_addr(&B.steps_empty[step_slot.at]), step_slot.phase ^ 1u, abort_ptr);
@@ -268,6 +258,22 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     ++issued;
                     slot.step(RING);
                 }
+                if (!ok || t > w.tile) continue;
+                // queries, behind the first keys and values: those need not wait until the last item's have been read
+                const int buffer = items % S::Q_BUFFERS;
+                ok = mbar_wait_warp(ptx::smem_addr(&B.q_empty[buffer]), (uint32_t)(items / S::Q_BUFFERS & 1) ^ 1u, abort_ptr);
+                if (!ok) break;
+                ++items;
+                if (ptx::elect_one()) {
+                    const uint32_t bar = ptx::smem_addr(&B.q_full[buffer]);
+                    const int second = w.p * P.plan.tile_tokens + P.half_tokens < w.s.queries ? 2 : 1;
+                    ptx::mbar_arrive_expect_tx(bar, second * LINES * P.box_rows * 128);
+                    for (int x = 0; x < second; ++x)
+                        for (int i = 0; i < LINES; ++i)
+                            ptx::tma_load_4d(smem + (2 * buffer + x) * S::OPERAND + i * 16384, &map_q, bar, 0, w.h * P.plan.group,
+                                             w.s.first + w.p * P.plan.tile_tokens + x * P.half_tokens, i);
+                }
+                __syncwarp();
             }
         }
         if (!ok) {                                                      // copies in flight are given a bounded chance to land
@@ -280,15 +286,18 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             };
             drain(full, slot, RING, issued);
             if (CODES) drain(B.steps_full, step_slot, PT_STEP_SLOTS, steps_issued);
-            for (int spin = 0; items > 0 && spin < (1 << 16) && !ptx::mbar_try_wait(ptx::smem_addr(&B.q_full), (uint32_t)(items - 1) & 1u); ++spin) {}
+            for (int k = 1; k <= S::Q_BUFFERS && k <= items; ++k)
+                for (int spin = 0; spin < (1 << 16) && !ptx::mbar_try_wait(ptx::smem_addr(&B.q_full[(items - k) % S::Q_BUFFERS]),
+                                                                           (uint32_t)((items - k) / S::Q_BUFFERS) & 1u); ++spin) {}
         }
     } else if (warp == PT_MMA) {
         // ---- products: P V of a tile and Q K^T of the next, one half after the other ------------------------------------------
         TileRing r;                                                     // the next entry of the ring: keys of the first tile, values, keys, ...
         uint32_t items = 0, n_p[2] = {0, 0};
         const uint32_t idesc_qk = ptx::idesc_f16(128, PT_KEYS, BF16, 0), idesc_pv = ptx::idesc_f16(128, D, std::is_same<M, __nv_bfloat16>::value, 1);
+        uint32_t q_at = 0;                                              // this item's query buffer
         auto issue_qk = [&](int x, int at) {
-            const uint64_t a = ptx::smem_desc(smem + x * S::OPERAND, 16, 1024, ptx::SWIZZLE_128B);
+            const uint64_t a = ptx::smem_desc(smem + (2 * q_at + x) * S::OPERAND, 16, 1024, ptx::SWIZZLE_128B);
             const uint64_t b = ptx::smem_desc(ring + at * S::OPERAND, 16, 1024, ptx::SWIZZLE_128B);
             if (ptx::elect_one()) {
 #pragma unroll
@@ -300,7 +309,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         };
         for (; ok && w.more(); w.next(P.plan)) {
             const Half half[2] = {half_of(P, w, 0), half_of(P, w, 1)};
-            ok = mbar_wait_warp(ptx::smem_addr(&B.q_full), items & 1u, abort_ptr) && mbar_wait_warp(ptx::smem_addr(&B.full[r.at]), r.phase, abort_ptr);
+            q_at = items % S::Q_BUFFERS;
+            ok = mbar_wait_warp(ptx::smem_addr(&B.q_full[q_at]), items / S::Q_BUFFERS & 1u, abort_ptr) && mbar_wait_warp(ptx::smem_addr(&B.full[r.at]), r.phase, abort_ptr);
             if (!ok) break;
             ++items;
             ptx::tc_fence_after();
@@ -318,7 +328,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int valid = w.s.length - (w.first + t * PT_KEYS);
                 if (!CODES && valid < PT_KEYS) {
                     // places behind the length: zeros instead of whatever lies there (NaN times a probability of 0)
-                    uint8_t* const v = gen + 2 * S::OPERAND + r.at * S::OPERAND;
+                    uint8_t* const v = gen + 2 * S::Q_BUFFERS * S::OPERAND + r.at * S::OPERAND;
                     for (int i = max(valid, 0) * 8 + lane; i < PT_KEYS * 8; i += 32)
 #pragma unroll
                         for (int line = 0; line < LINES; ++line) *reinterpret_cast<uint4*>(v + line * 16384 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -328,11 +338,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 bool have_keys = false;
                 for (int x = 0; ok && x < 2; ++x) {
                     if (t >= half[x].from && t < half[x].to) {
+                        const uint64_t b = ptx::smem_desc(ring + r.at * S::OPERAND, 16384, 1024, ptx::SWIZZLE_128B);
                         ok = mbar_wait_warp(ptx::smem_addr(&B.p_full[x]), n_p[x] & 1u, abort_ptr);
                         if (!ok) break;
-                        ++n_p[x];
                         ptx::tc_fence_after();
-                        const uint64_t b = ptx::smem_desc(ring + r.at * S::OPERAND, 16384, 1024, ptx::SWIZZLE_128B);
                         if (ptx::elect_one()) {
 #pragma unroll
                             for (int i = 0; i < PT_KEYS / 16; ++i)
@@ -340,6 +349,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             ptx::mma_commit(ptx::smem_addr(&B.pv_done[x]));
                         }
                         __syncwarp();
+                        ++n_p[x];
                     }
                     if (more && t + 1 >= half[x].from && t + 1 < half[x].to) {
                         if (!have_keys) ok = mbar_wait_warp(ptx::smem_addr(&B.full[next.at]), next.phase, abort_ptr);
@@ -359,7 +369,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 r.step(S::SLOTS);
                 if (more) r.step(S::SLOTS);
             }
-            if (ok && ptx::elect_one()) ptx::mma_commit(ptx::smem_addr(&B.q_empty));
+            if (ok && ptx::elect_one()) ptx::mma_commit(ptx::smem_addr(&B.q_empty[q_at]));
             __syncwarp();
         }
         // tensor memory is given back when nothing writes to it any more
@@ -375,7 +385,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                      mbar_wait_warp(ptx::smem_addr(&B.empty[slot.at]), slot.phase ^ 1u, abort_ptr);
                 if (!ok) break;
                 const uint8_t* const from = gen + (raw_ring - smem) + raw.at * S::RAW;
-                uint8_t* const to = gen + 2 * S::OPERAND + slot.at * S::OPERAND;
+                uint8_t* const to = gen + 2 * S::Q_BUFFERS * S::OPERAND + slot.at * S::OPERAND;
                 if (i & 1) expand_code_row<D, __half>(from, to, row);   // values
                 else expand_code_row<D, T>(from, to, row);
                 ptx::fence_proxy_async_smem();
@@ -411,6 +421,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     ptx::tc_fence_after();
                     const int key0 = w.first + t * PT_KEYS, lo = low - key0, hi = high - key0;
                     const bool edge = key0 < half.low_last || key0 + PT_KEYS > half.high_first;
+                    // the tile's scores, two blocks of 32 at a time, and read twice (all 128 in registers: 4 % slower)
                     uint32_t v[2][32];
                     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     ptx::tmem_ld32(t_s, v[0]);
@@ -418,8 +429,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int k = 0; k < 4; ++k) {
                         ptx::tmem_ld_wait();
                         if (k < 3) ptx::tmem_ld32(t_s + 32 * (k + 1), v[(k + 1) & 1]);
-                        if (edge) tile_max<CODES, true>(v[k & 1], f + 32 * k, lo - 32 * k, hi - 32 * k, top);
-                        else tile_max<CODES, false>(v[k & 1], f + 32 * k, 0, 32, top);
+                        if (edge) tile_max<CODES, true>(v[k & 1], f + 32 * k, seen_bits(lo - 32 * k, hi - 32 * k), top);
+                        else tile_max<CODES, false>(v[k & 1], f + 32 * k, 0u, top);
                     }
                     const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * P.c;
                     uint32_t larger = unit;
@@ -448,12 +459,13 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             ok = mbar_wait_warp(ptx::smem_addr(&B.pv_done[x]), (n_s - 1) & 1u, abort_ptr);
                             ptx::tc_fence_after();
 #pragma unroll 1
-                            for (int k = 0; k < D; k += 32) {
-                                ptx::tmem_ld32(t_o + k, v[0]);
+                            for (int k = 0; k < D; k += 16) {
+                                uint32_t old[16];
+                                ptx::tmem_ld16(t_o + k, old);
                                 ptx::tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) v[0][e] = __float_as_uint(__uint_as_float(v[0][e]) * factor);
-                                ptx::tmem_st32(t_o + k, v[0]);
+                                for (int e = 0; e < 16; ++e) old[e] = __float_as_uint(__uint_as_float(old[e]) * factor);
+                                ptx::tmem_st16(t_o + k, old);
                             }
                             ptx::tmem_st_wait();
                         }
@@ -466,8 +478,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         ptx::tmem_ld_wait();
                         if (k < 3) ptx::tmem_ld32(t_s + 32 * (k + 1), v[(k + 1) & 1]);
                         uint32_t p[16];
-                        if (edge) tile_probabilities<M, CODES, true>(v[k & 1], f + 32 * k, up, c2, minus_base, lo - 32 * k, hi - 32 * k, sum, p);
-                        else tile_probabilities<M, CODES, false>(v[k & 1], f + 32 * k, up, c2, minus_base, 0, 32, sum, p);
+                        if (edge) {
+                            const uint32_t seen = seen_bits(lo - 32 * k, hi - 32 * k);
+                            tile_probabilities<M, CODES, true>(v[k & 1], f + 32 * k, seen, up, c2, minus_base, sum, p);
+                        } else {
+                            tile_probabilities<M, CODES, false>(v[k & 1], f + 32 * k, 0u, up, c2, minus_base, sum, p);
+                        }
                         ptx::tmem_st16(t_s + 16 * k, p);                // (columns whose scores have been read)
                     }
                     ptx::tmem_st_wait();
@@ -551,20 +567,33 @@ paged_tiles_join_kernel(const __grid_constant__ TilesParams P) {
     const JoinNote n = P.notes[blockIdx.x + 1];
     if (n.last_cta < 0) return;
     const int x = blockIdx.y >> 2, col0 = (blockIdx.y & 3) * COLS, row = threadIdx.x;
-    const Sequence s = sequence_of(P.plan.seq, n.b);
+    const Sequence s{n.length, n.first, n.queries};
     const int i0 = n.p * P.plan.tile_tokens + x * P.half_tokens, rows = min(P.half_tokens, s.queries - i0) * P.plan.group;
     if (row >= rows) return;
     float o[COLS], m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int k = 0; k < COLS; ++k) o[k] = 0.0f;
-    for (int cta = n.first_cta; cta <= n.last_cta; ++cta) {
-        const float* const part = P.partial + (2ll * cta + (cta == n.first_cta ? 1 : 0)) * PART + x * (D + 2) * 128 + row;
-        const float pm = part[D * 128], pl = part[(D + 1) * 128], top = fmaxf(m, pm), base = top == -INFINITY ? 0.0f : top;
-        const float mine = exp2_approx(m - base), theirs = exp2_approx(pm - base);
-        m = top;
-        l = l * mine + pl * theirs;
+    for (int cta = n.first_cta; cta <= n.last_cta; cta += 2) {           // two parts' loads under way at once
+        float v[2][COLS], pm[2], pl[2];
 #pragma unroll
-        for (int k = 0; k < COLS; ++k) o[k] = o[k] * mine + part[(col0 + k) * 128] * theirs;
+        for (int i = 0; i < 2; ++i) {
+            pm[i] = -INFINITY;
+            pl[i] = 0.0f;
+            const bool there = cta + i <= n.last_cta;
+            const float* const part = P.partial + (2ll * (cta + i) + (cta + i == n.first_cta ? 1 : 0)) * PART + x * (D + 2) * 128 + row;
+            if (there) { pm[i] = part[D * 128]; pl[i] = part[(D + 1) * 128]; }
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) v[i][k] = there ? part[(col0 + k) * 128] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float top = fmaxf(m, pm[i]), base = top == -INFINITY ? 0.0f : top;
+            const float mine = exp2_approx(m - base), theirs = exp2_approx(pm[i] - base);
+            m = top;
+            l = l * mine + pl[i] * theirs;
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) o[k] = o[k] * mine + v[i][k] * theirs;
+        }
     }
     const int i = row / P.plan.group, head = n.h * P.plan.group + row - i * P.plan.group;
     const long long token = s.first + i0 + i;

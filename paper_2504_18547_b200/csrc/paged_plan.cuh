@@ -61,7 +61,9 @@ __device__ __forceinline__ int sequence_tiles(const PlanParams& A, int b, bool& 
     if (b < A.seq.sequences) s = sequence_of(A.seq, b, ok);
     const int runs = b < A.seq.sequences ? Runs::runs(A, s) : 0, same = runs ? Runs::uniform(A, s) : 1;
     int sum = runs * same, first;
-    uint32_t many = __ballot_sync(0xffffffffu, same == 0);
+    if (same == 0 && runs <= 16)
+        for (int p = 0; p < runs; ++p) sum += Runs::tiles(A, s, p, first);
+    uint32_t many = __ballot_sync(0xffffffffu, same == 0 && runs > 16);
     const int lane = threadIdx.x & 31;
     while (many) {                                                     // the warp's lanes take a sequence's runs
         const int from = __ffs(many) - 1;
@@ -200,17 +202,20 @@ private:
 // at slot 2c (CTA c began inside the item) and 2c + 1 (the item began in CTA c's stretch and did not end there).
 struct JoinNote {
     int first_cta, last_cta;   // last_cta < 0: nothing to do
-    int b, h, p, pad_[3];
+    int b, h, p;
+    int length, first, queries;   // the sequence
 };
 
 // Written by every CTA: the CTA behind an item's first one names it.
-__device__ __forceinline__ JoinNote join_note(const Stretch& r, int cta) {
+__device__ __forceinline__ JoinNote join_note(const PlanParams& A, const Stretch& r, int cta) {
     JoinNote n{};
     n.last_cta = -1;
     if (r.count > 0 && r.tile > 0 && r.first_cta == cta - 1) {
         n.first_cta = r.first_cta;
         n.last_cta = r.last_cta;
         n.b = r.b; n.h = r.h; n.p = r.p;
+        const Sequence s = sequence_of(A.seq, r.b);
+        n.length = s.length; n.first = s.first; n.queries = s.queries;
     }
     return n;
 }

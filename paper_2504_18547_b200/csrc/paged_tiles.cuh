@@ -91,6 +91,12 @@ __device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
     b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
 }
 
+// Bits of the columns of a block of 32 that a row sees: low <= column < high.
+__device__ __forceinline__ uint32_t seen_bits(int low, int high) {
+    const uint32_t below_high = high >= 32 ? 0xFFFFFFFFu : high <= 0 ? 0u : (1u << high) - 1u;
+    return low >= 32 ? 0u : low <= 0 ? below_high : below_high & ~((1u << low) - 1u);
+}
+
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                  : "memory");

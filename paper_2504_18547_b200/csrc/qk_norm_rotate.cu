@@ -64,6 +64,15 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 template <int LANES>
+__device__ __forceinline__ void row_sums(float& a, float& b) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        const float x = __shfl_xor_sync(0xffffffffu, a, o), y = __shfl_xor_sync(0xffffffffu, b, o);
+        a += x;
+        b += y;
+    }
+}
+template <int LANES>
 __device__ __forceinline__ float row_max(float v) {
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -72,7 +81,7 @@ __device__ __forceinline__ float row_max(float v) {
 
 // TI: input type, TO: type of q_out, k_out and of a 16-bit cache, CODES: the cache holds 8-bit codes.
 template <int D, typename TI, typename TO, bool CODES>
-__global__ void __launch_bounds__(QN_THREADS)
+__global__ void __launch_bounds__(QN_THREADS, 4)
 qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pairs) {
     constexpr int LANES = D / 8, ROWS = QN_THREADS / LANES;              // threads of a head row, rows that a block walks side by side
     __shared__ float2 turn[D / 2];                                       // (cos, sin) of the token's angles
@@ -125,19 +134,27 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pair
                     load8<float>(gain + c0, g);
                     if (offset) load8<float>(offset + c0, o);
                 }
-                float mean = 0.0f;
+                // Mean and variance in one pass: sums of x - x0 and of its square, x0 the row's first channel.  The variance is the mean square less
+                // the mean's, which x0 costs at most a factor D in precision: no channel is more than sqrt(D) deviations away from the mean.
+                float mean = 0.0f, v;
                 if (norm == VITINT_NORM_LAYER) {
-                    float s = 0.0f;
+                    const float x0 = __shfl_sync(0xffffffffu, y[0], sub);
+                    float s = 0.0f, q = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s += y[i];
-                    mean = row_sum<LANES>(s) * (1.0f / D);
+                    for (int i = 0; i < 8; ++i) { const float d = y[i] - x0; s += d; q = fmaf(d, d, q); }
+                    row_sums<LANES>(s, q);
+                    s *= 1.0f / D;
+                    mean = x0 + s;
+                    v = fmaxf(fmaf(-s, s, q * (1.0f / D)), 0.0f) + P.eps;
+                } else {
+                    float q = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q = fmaf(y[i], y[i], q);
+                    v = fmaf(row_sum<LANES>(q), 1.0f / D, P.eps);
                 }
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { const float d = y[i] - mean; s = fmaf(d, d, s); }
                 // 1 / sqrt by the hardware's approximation and a Newton step (0 and infinity stay what the approximation makes of them)
-                const float v = row_sum<LANES>(s) * (1.0f / D) + P.eps;
-                float r = rsqrtf(v);
+                float r;
+                asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
                 if (v > 1e-36f && v < 1e36f) r = r * fmaf(-0.5f * v * r, r, 1.5f);
                 if (live && !is_v) {
 #pragma unroll
@@ -175,7 +192,7 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pair
             float m = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y[i]));
-            step = __fdiv_rn(row_max<LANES>(m), 127.0f);
+            step = row_max<LANES>(m) * (1.0f / 127.0f);
         }
         if (!live) continue;
         if (is_q) {
@@ -188,9 +205,10 @@ qk_norm_rotate_kernel(const __grid_constant__ RotateParams P, int norm, int pair
         void* const base = is_v ? P.cache_v : P.cache_k;
         if (CODES) {
             uint32_t w[2] = {0u, 0u};
-            // the quotient by the step's reciprocal; at most 127 (1 + 2^-22), which needs no clamp, unless the step is denormal
+            // the quotient by the step's reciprocal; at most 127 (1 + 2^-21), which needs no clamp, unless the step is denormal
             if (step >= 1e-37f) {
-                const float r = __frcp_rn(step);
+                float r;
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(step));
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t u[4];
