@@ -571,7 +571,7 @@ int vitint_cache_weigh(const void* q, int32_t q_type, int64_t tokens, int32_t q_
  *     the batch's page table uses and none is named twice.
  *   kept: device int32 [sequences][kv_heads][budget], the indices kept, -1 behind them.  counts: device int32 [sequences],
  *     min(length, budget): the new lengths.  counts is not batch->lengths.
- *   batch: query_starts and max_queries are not used.  sinks + recent <= budget.
+ *   batch: query_starts and max_queries are not used.  sinks + recent <= budget.  At most 65,535 sequences times heads.
  *   Page indexes outside the cache, and lengths beyond the batch's bounds, are not followed and make the next
  *     vitint_device_status() return VITINT_ERR_INVALID_ARG.
  *   Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA. */

@@ -14,6 +14,7 @@ namespace vitint {
 constexpr int64_t CACHE_MAX_LENGTH = 1ll << 29;
 
 inline bool aligned16_elements(int64_t n, int size) { return (n * size) % 16 == 0; }
+inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline int dtype_bytes(int type) { return type == VITINT_F32 ? 4 : type == VITINT_I8 ? 1 : 2; }
 
 inline int check_cache(const vitint_cache* c) {
@@ -39,6 +40,7 @@ inline int check_batch(const vitint_cache* c, const vitint_cache_batch* b, bool 
     if (!b || !b->page_table || !b->lengths || b->sequences <= 0 || b->table_stride <= 0) return VITINT_ERR_INVALID_ARG;
     if (queries && (!b->query_starts || b->max_queries <= 0)) return VITINT_ERR_INVALID_ARG;
     if (b->max_length <= 0) return VITINT_ERR_INVALID_ARG;
+    if (!aligned_to(b->page_table, 4) || !aligned_to(b->lengths, 4) || !aligned_to(b->query_starts, 4)) return VITINT_ERR_ALIGNMENT;
     if (b->max_length > CACHE_MAX_LENGTH || b->sequences > 65535) return VITINT_ERR_UNSUPPORTED;
     if ((b->max_length + c->page_tokens - 1) / c->page_tokens > b->table_stride) return VITINT_ERR_INVALID_ARG;
     return VITINT_OK;

@@ -337,6 +337,7 @@ extern "C" int vitint_cache_evict(const vitint_cache* cache, const vitint_cache_
     if (int rc = check_cache(cache)) return rc;
     if (int rc = check_batch(cache, batch, false)) return rc;
     if (!weights || !new_table || !kept || !counts || counts == batch->lengths || new_table == batch->page_table) return VITINT_ERR_INVALID_ARG;
+    if (!aligned_to(weights, 4) || !aligned_to(new_table, 4) || !aligned_to(kept, 4) || !aligned_to(counts, 4)) return VITINT_ERR_ALIGNMENT;
     if (budget <= 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return VITINT_ERR_INVALID_ARG;
     if (new_table_stride <= 0 || ((int64_t)budget + cache->page_tokens - 1) / cache->page_tokens > new_table_stride) return VITINT_ERR_INVALID_ARG;
     if (budget > CACHE_MAX_LENGTH) return VITINT_ERR_UNSUPPORTED;

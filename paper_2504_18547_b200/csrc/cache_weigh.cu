@@ -424,6 +424,7 @@ extern "C" int vitint_cache_weigh(const void* q, int32_t q_type, int64_t tokens,
                                   void* stream) {
     if (int rc = check_paged_queries(q, q_type, tokens, q_heads, q_token_stride, q_head_stride, cache, batch, scale, causal, window)) return rc;
     if (!lse || !weights_out) return VITINT_ERR_INVALID_ARG;
+    if (!aligned_to(lse, 4) || !aligned_to(weights_in, 4) || !aligned_to(weights_out, 4)) return VITINT_ERR_ALIGNMENT;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < vitint_cache_weigh_workspace_bytes(cache, batch))
         return VITINT_ERR_WORKSPACE;
     WeighParams P{};

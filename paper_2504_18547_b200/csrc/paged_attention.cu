@@ -34,8 +34,10 @@ struct RowsShape {
     static constexpr int HALF = KT * ROW;                              // bytes of a tile's keys (or values)
     static constexpr int STEPS = CODES ? KT * 4 : 0;                   // bytes of a tile's key (or value) steps
     static constexpr int STAGE = 2 * HALF;
-    static constexpr int CTAS = NQ == 1 ? 3 : 2;                       // on an SM
-    static constexpr int STAGES = (NQ == 1 ? 2 : 3) * 32768 / STAGE + (CODES && NQ == 2 ? -1 : 0);
+    // CTAs on an SM, and tiles in a CTA's ring.  Codes are bound by latency as much as by bytes (they are half of them, and expanded): more CTAs
+    // with fewer tiles (64 sequences of up to 6001 tokens: three CTAs of four tiles 95 us, four of two 85).
+    static constexpr int CTAS = NQ == 2 ? 2 : CODES ? 4 : 3;
+    static constexpr int STAGES = CODES ? (NQ == 2 ? 5 : 2) : (NQ == 2 ? 3 : 2);
     static constexpr int NREG = NQ * D / 4;                            // a thread's outputs
     static constexpr int PART = NREG * 32 + NQ * 16;                   // floats of a partial result: a warp's output fragments, maxima and sums of the rows
     static constexpr int MERGE = 2 * PART * 4;
@@ -650,7 +652,7 @@ paged_rows_join_kernel(const __grid_constant__ RowsParams P) {
     if (mt == 0) write_lse<NQ>(P, s, note.h, note.p, m, l);
 }
 
-inline int rows_grid(int nq) { return (nq == 1 ? 3 : 2) * sm_count(); }
+inline int rows_grid(int nq) { return (nq == 1 ? 4 : 2) * sm_count(); }      // at most
 inline size_t rows_partial_bytes(int nq, int head_dim) { return (size_t)rows_grid(nq) * 2 * (nq * head_dim * 8 + nq * 16) * 4; }
 
 template <int D, typename T, bool CODES, int NQ>
@@ -662,7 +664,7 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + S::KT - 1) / S::KT;
     const long long items = (long long)batch->sequences * cache->kv_heads * runs;
     if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
-    int grid = rows_grid(NQ);
+    int grid = S::CTAS * sm_count();
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
     P.partial = (float*)((uint8_t*)workspace + notes_bytes(rows_grid(NQ)));
@@ -708,7 +710,7 @@ extern "C" int vitint_paged_attention(const void* q, int32_t q_type, int64_t tok
                                       float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = check_paged_queries(q, q_type, tokens, q_heads, q_token_stride, q_head_stride, cache, batch, scale, causal, window)) return rc;
     if (!out) return VITINT_ERR_INVALID_ARG;
-    if (!aligned16(out) || out_token_stride % 8 != 0 || out_head_stride % 8 != 0) return VITINT_ERR_ALIGNMENT;
+    if (!aligned16(out) || !aligned_to(lse, 4) || out_token_stride % 8 != 0 || out_head_stride % 8 != 0) return VITINT_ERR_ALIGNMENT;
     if (out_token_stride <= 0 || out_head_stride < cache->head_dim) return VITINT_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
         workspace_bytes < vitint_paged_attention_workspace_bytes(q_heads, cache, batch))

@@ -275,9 +275,10 @@ extern "C" int vitint_qk_norm_rotate(const vitint_qk_norm_rotate_desc* d, const 
         return VITINT_ERR_INVALID_ARG;
     }
     const int in = dtype_bytes(d->in_type);
-    const void* pointers[8] = {d->q, d->k, d->v, d->q_gain, d->k_gain, d->q_offset, d->k_offset, nullptr};
+    const void* pointers[7] = {d->q, d->k, d->v, d->q_gain, d->k_gain, d->q_offset, d->k_offset};
     for (const void* p : pointers) if (!aligned16(p)) return VITINT_ERR_ALIGNMENT;
     if (!aligned16(d->q_out) || !aligned16(d->k_out)) return VITINT_ERR_ALIGNMENT;
+    if (!aligned_to(d->positions, 4) || !aligned_to(d->frequencies, 8) || !aligned_to(d->slots, 8) || !aligned_to(d->weights, 4)) return VITINT_ERR_ALIGNMENT;
     const int64_t q_width = (int64_t)d->q_heads * d->head_dim, k_width = (int64_t)d->kv_heads * d->head_dim;
     struct { bool used; int64_t stride, width; int size; } rows[5] = {
         {d->q != nullptr, d->q_stride, q_width, in}, {true, d->k_stride, k_width, in}, {d->v != nullptr, d->v_stride, k_width, in},

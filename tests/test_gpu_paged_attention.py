@@ -259,3 +259,20 @@ def test_chunk_tiny_value_steps_in_fp16():
     want = list(pu.attention64(q, cache, table, [1000], starts, 0.08, True, 0))
     want[2] += 2.0 ** -25
     pu.check_attention(out, lse, want)
+
+
+@pytest.mark.parametrize("new", [1, 23])
+def test_many_sequences(new):
+    """More sequences than lanes of a warp, some without new tokens: the plan walks them in blocks of 32."""
+    seqs = [((37 * i) % 150 + new, new if i % 7 else 0) for i in range(101)]
+    run_case(50, 64, 16, BF16, BF16, 2, 2, seqs)
+
+
+def test_queries_over_themselves():
+    """The output may be the queries' memory: an item's queries are read before its rows are written."""
+    g = torch.Generator().manual_seed(51)
+    for seqs in (((90, 1), (5000, 1)), ((90, 30), (2000, 77))):
+        cache, table, lengths, starts, q, batch = _small(g, seqs)
+        gpu, qd = pu.to_gpu(cache), q.cuda()
+        want = vt.vitint_paged_attention(qd, gpu, batch, 0.09).clone()
+        assert torch.equal(vt.vitint_paged_attention(qd, gpu, batch, 0.09, out=qd), want)

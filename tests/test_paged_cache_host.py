@@ -40,7 +40,7 @@ CACHE_FAULTS = [(dict(k=0), INVALID), (dict(v=0), INVALID), (dict(pages=0), INVA
                 (dict(pages=1 << 31), UNSUPPORTED), (dict(type=I8, k_steps=FAKE + 4, v_steps=FAKE), ALIGNMENT), (dict(type=I8, k_steps=FAKE), INVALID)]
 BATCH_FAULTS = [(dict(table=0), INVALID), (dict(lengths=0), INVALID), (dict(starts=0), INVALID), (dict(sequences=0), INVALID), (dict(max_queries=0), INVALID),
                 (dict(max_length=0), INVALID), (dict(max_length=129), INVALID), (dict(stride=0), INVALID), (dict(sequences=70000), UNSUPPORTED),
-                (dict(max_length=1 << 30, stride=1 << 30), UNSUPPORTED)]
+                (dict(max_length=1 << 30, stride=1 << 30), UNSUPPORTED), (dict(lengths=FAKE + 2), ALIGNMENT), (dict(table=FAKE + 1), ALIGNMENT)]
 
 
 @pytest.mark.parametrize("change,status", CACHE_FAULTS)
@@ -67,7 +67,7 @@ def test_batch_faults(B, change, status):
     (dict(scale=float("nan")), INVALID), (dict(causal=2), INVALID), (dict(window=-1), INVALID), (dict(causal=0, window=4), INVALID), (dict(q=FAKE + 8), ALIGNMENT),
     (dict(q_token=1028), ALIGNMENT), (dict(q_head=130), ALIGNMENT), (dict(q_head=64), INVALID), (dict(q_token=0), INVALID), (dict(out=FAKE + 4), ALIGNMENT),
     (dict(out_token=1001), ALIGNMENT), (dict(out_head=64), INVALID), (dict(out_token=-1024), INVALID), (dict(), WORKSPACE), (dict(workspace=FAKE), WORKSPACE),
-    (dict(workspace=FAKE + 16, size=1 << 30), WORKSPACE), (dict(tokens=1 << 25), UNSUPPORTED)])
+    (dict(workspace=FAKE + 16, size=1 << 30), WORKSPACE), (dict(tokens=1 << 25), UNSUPPORTED), (dict(lse=FAKE + 2), ALIGNMENT)])
 def test_attention_faults(B, change, status):
     assert attention(B, **change) == status
 
@@ -81,7 +81,7 @@ def test_weigh_faults(B):
 @pytest.mark.parametrize("change,status", [
     (dict(weights=None), INVALID), (dict(kept=None), INVALID), (dict(counts=None), INVALID), (dict(table=None), INVALID), (dict(budget=0), INVALID), (dict(budget=-4), INVALID),
     (dict(sinks=-1), INVALID), (dict(recent=-1), INVALID), (dict(sinks=9, recent=8), INVALID), (dict(sinks=2 ** 31 - 1, recent=2 ** 31 - 1), INVALID), (dict(stride=0), INVALID),
-    (dict(budget=17), INVALID), (dict(counts=FAKE), INVALID), (dict(table=FAKE), INVALID)])
+    (dict(budget=17), INVALID), (dict(counts=FAKE), INVALID), (dict(table=FAKE), INVALID), (dict(kept=FAKE + 2), ALIGNMENT), (dict(weights=FAKE + 1), ALIGNMENT)])
 def test_evict_faults(B, change, status):
     f = dict(cache=cache(B), batch=batch(B), weights=FAKE, budget=16, sinks=0, recent=0, table=FAKE + 64, stride=1, kept=FAKE, counts=FAKE + 4096, stream=None) | change
     assert B.lib().vitint_cache_evict(*f.values()) == status
@@ -101,7 +101,8 @@ def rotate(B, c=None, **change):
     (dict(frequencies=0), INVALID), (dict(k_gain=0), INVALID), (dict(q_gain=0), INVALID), (dict(norm=0), INVALID), (dict(k_offset=FAKE), INVALID), (dict(eps=-1.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(v=0), INVALID), (dict(slots=0), INVALID), (dict(q=FAKE + 8), ALIGNMENT), (dict(k=FAKE + 4), ALIGNMENT), (dict(q_stride=1025), ALIGNMENT),
     (dict(k_stride=200), INVALID), (dict(q_out_stride=512), INVALID), (dict(q_gain=FAKE + 4), ALIGNMENT), (dict(k_out=FAKE, k_out_stride=256, in_type=F32), INVALID),
-    (dict(q_out_stride=1024), INVALID), (dict(tokens=1 << 25), UNSUPPORTED)])
+    (dict(q_out_stride=1024), INVALID), (dict(tokens=1 << 25), UNSUPPORTED), (dict(slots=FAKE + 4), ALIGNMENT), (dict(frequencies=FAKE + 4), ALIGNMENT),
+    (dict(positions=FAKE + 2), ALIGNMENT)])
 def test_rotate_faults(B, change, status):
     if "k_out" in change:
         change = change | dict(k=FAKE)
