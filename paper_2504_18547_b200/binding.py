@@ -714,13 +714,19 @@ class CacheBatch:
     max_length: int
 
     def desc(self, where: str = "CacheBatch", device: int | None = None, page_tokens: int = 128) -> bytes:
-        table, starts = self.page_table, self.query_starts
+        table, lengths, starts = self.page_table, self.lengths, self.query_starts
         device = _cuda_device() if device is None else device
-        n, entries = _table(table, self.lengths.numel(), device, where, "page_table")
-        if not (0 <= self.max_queries < 1 << 31 and 0 < self.max_length <= table.shape[1] * page_tokens):
+        i32, shape, n = torch.int32, table.shape, lengths.numel()
+        if (table.dtype is not i32 or len(shape) != 2 or shape[0] != n or table.get_device() != device or lengths.dtype is not i32
+                or lengths.get_device() != device or not lengths.is_contiguous()):
+            _require(False, where, "page_table and lengths are int32 tensors [sequences, entries] and [sequences] on the current device")
+        stride = table.stride()
+        if shape[1] > 1 and stride[1] != 1:
+            _require(False, where, "a row's entries of page_table lie behind one another")
+        if not (0 <= self.max_queries < 1 << 31 and 0 < self.max_length <= shape[1] * page_tokens):
             _require(False, where, "max_queries and max_length are counts, and the page table holds max_length tokens")
-        return _PACK_BATCH(table.data_ptr(), entries, _array(self.lengths, torch.int32, n, device, where, "lengths"),
-                           0 if starts is None else _array(starts, torch.int32, n + 1, device, where, "query_starts"), n, self.max_queries, self.max_length)
+        return _PACK_BATCH(table.data_ptr(), stride[0] if n > 1 else shape[1], lengths.data_ptr(),
+                           0 if starts is None else _array(starts, i32, n + 1, device, where, "query_starts"), n, self.max_queries, self.max_length)
 
 
 def _table(t, n: int, device: int, where: str, name: str):

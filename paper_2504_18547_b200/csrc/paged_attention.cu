@@ -664,6 +664,7 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + S::KT - 1) / S::KT;
     const long long items = (long long)batch->sequences * cache->kv_heads * runs;
     if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
+    P.plan.whole = tiles <= WHOLE_TILES_ROWS;
     int grid = S::CTAS * sm_count();
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
@@ -677,7 +678,7 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     }
     launch_kernel(paged_rows_kernel<D, T, CODES, NQ>, dim3(grid), dim3(PA_THREADS), S::SMEM, st, map_k, map_v, P);
     if (int rc = cuda_status(cudaGetLastError())) return rc;
-    if (tiles > 1 && grid > 1) launch_kernel(paged_rows_join_kernel<D, T, CODES, NQ>, dim3(grid - 1), dim3(D * 2), 0, st, P);
+    if (!P.plan.whole && grid > 1) launch_kernel(paged_rows_join_kernel<D, T, CODES, NQ>, dim3(grid - 1), dim3(D * 2), 0, st, P);
     return cuda_status(cudaGetLastError());
 }
 

@@ -626,6 +626,7 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
     const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + PT_KEYS - 1) / PT_KEYS;
     const long long items = (long long)batch->sequences * cache->kv_heads * runs;
     if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
+    P.plan.whole = tiles <= WHOLE_TILES_CHUNKS;
     int grid = sm_count();
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
@@ -639,7 +640,7 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
     }
     launch_kernel(paged_tiles_kernel<D, T, CODES>, dim3(grid), dim3(S::THREADS), S::SMEM, st, map_q, map_k, map_v, P);
     if (int rc = cuda_status(cudaGetLastError())) return rc;
-    if (tiles > 1 && grid > 1) launch_kernel(paged_tiles_join_kernel<D, T>, dim3(grid - 1, 8), dim3(128), 0, st, P);
+    if (!P.plan.whole && grid > 1) launch_kernel(paged_tiles_join_kernel<D, T>, dim3(grid - 1, 8), dim3(128), 0, st, P);
     return cuda_status(cudaGetLastError());
 }
 
