@@ -86,7 +86,7 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
     extern __shared__ uint32_t ev_keys[];
     __shared__ __align__(16) uint32_t bins[2][EV_BINS];                // the largest digit first
     __shared__ unsigned long long warp_sums[32];
-    __shared__ uint32_t found[2];                                      // the digit, and how many are still wanted inside it
+    __shared__ uint32_t found[3];                                      // the digit, how many are still wanted inside it, and how many it has
     __shared__ uint32_t larger_of[33], equal_of[33];                   // counts of the block's warps, then of the block
     const int blocks = (int)cluster_size(), rank = (int)cluster_rank();
     const int h = blockIdx.x / blocks, b = blockIdx.y, t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -179,20 +179,22 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
         const uint32_t count_of[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (above < want && want <= above + count_of[k]) { found[0] = digits - (uint32_t)(4 * t + k); found[1] = want - above; }
+            if (above < want && want <= above + count_of[k]) { found[0] = digits - (uint32_t)(4 * t + k); found[1] = want - above; found[2] = count_of[k]; }
             above += count_of[k];
         }
         __syncthreads();
         prefix |= found[0] << low;
         known |= digits << low;
         want = found[1];
+        const bool all_stay = want == found[2];
         __syncthreads();
+        if (all_stay) break;                                           // (the same for all blocks: further digits tell nothing)
     }
-    // `prefix` is the last weight to stay, `want` of the tokens that have it do.  A warp has a run of the block's tokens, 32 at a time.
+    // Of the digits known, `prefix` are the last to stay, and `want` of the tokens that have them do.  A warp has a run of the block's tokens, 32 at a time.
     const int run = ((n + 1023) / 1024) * 32, from = min(warp * run, n), to = min(from + run, n);
     uint32_t larger = 0, equal = 0;
     for (int i = from + lane; i < to; i += 32) {
-        const uint32_t k = key_of(i);
+        const uint32_t k = key_of(i) & known;
         larger += k > prefix;
         equal += k == prefix;
     }
@@ -221,7 +223,7 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
     }
     for (int i0 = from; i0 < to; i0 += 32) {
         const int i = i0 + lane;
-        const uint32_t k = i < to ? key_of(i) : 0u;
+        const uint32_t k = i < to ? key_of(i) & known : 0u;
         const bool is_larger = i < to && k > prefix, is_equal = i < to && k == prefix;
         const uint32_t a = __ballot_sync(0xffffffffu, is_larger), e = __ballot_sync(0xffffffffu, is_equal), below = (1u << lane) - 1u;
         const uint32_t my_equal = ahead_equal + __popc(e & below);

@@ -13,6 +13,9 @@
 // takes its codes as they lie, sixteen bytes at a time.
 // Up to eight rows a probability is multiplied as the sum of two 16-bit numbers (the tensor core is idle otherwise), so that only the output is
 // rounded.
+//
+// One token each of 48 sequences with up to 8192 cached ones (32 query heads on 8 of 128, 680 MB): 115 us, 5.9 TB/s; 2 x 3 tokens over 131,072 (12
+// rows a head): 98 us, 5.5 TB/s; 64 sequences of codes (346 MB): 83 us, 4.2 TB/s (queries as rows, bf16 operands: 123).
 #include "paged_tiles.cuh"
 #include "paged_attention_tiles.cu"
 
