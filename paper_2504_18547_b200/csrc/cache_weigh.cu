@@ -360,7 +360,7 @@ inline int weigh_grid() { return 3 * sm_count(); }                     // (of fe
 template <int D, typename T, bool CODES, bool FEW>
 int cache_weigh_go(WeighParams& P, const CUtensorMap& map_q, const CUtensorMap& map_k, size_t smem, long long steps, cudaStream_t st) {
     // CTAs that fit an SM beside one another (FEW: barriers and the like take less than 2 KB)
-    const int fit = (int)(233472 / (smem + 3072));
+    const int fit = (int)(228 * 1024 / (smem + 3 * 1024));
     long long grid = (long long)(!FEW ? 1 : fit < (CODES ? 2 : 3) ? fit : (CODES ? 2 : 3)) * sm_count();
     if (grid > steps) grid = steps;
     const int dev = current_device();
