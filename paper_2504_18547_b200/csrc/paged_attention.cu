@@ -221,6 +221,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 ok = mbar_wait_warp(bars + 8 * (STAGES + stage), phase ^ 1u, abort_flag);
                 if (!ok) break;
                 const uint32_t full = bars + 8 * stage;
+                if (CODES && mine && !inside) zero_steps(pa_smem + STAGES * S::STAGE + stage * 2 * S::STEPS + lane * P.page_rows * 4, S::STEPS, P.page_rows);
+                __syncwarp();
                 if (lane == 0) ptx::mbar_arrive_expect_tx(full, 2u * n * copy_bytes + (CODES ? 2u * n_steps * P.page_rows * 4u : 0u));
                 __syncwarp();
                 if (mine) {

@@ -233,6 +233,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     ok = mbar_wait_warp(ptx::smem_addr(&B.steps_empty[step_slot.at]), step_slot.phase ^ 1u, abort_ptr);
                     if (!ok) break;
                     const uint32_t bar = ptx::smem_addr(&B.steps_full[step_slot.at]), to = ptx::smem_addr(&steps[step_slot.at][0]) + lane * P.page_rows * 4;
+                    if (mine && !inside) zero_steps(reinterpret_cast<uint8_t*>(&steps[step_slot.at][0]) + lane * P.page_rows * 4, PT_KEYS * 4, P.page_rows);
+                    __syncwarp();
                     if (lane == 0) ptx::mbar_arrive_expect_tx(bar, 2u * n_steps * P.page_rows * 4u);
                     __syncwarp();
                     if (inside) {

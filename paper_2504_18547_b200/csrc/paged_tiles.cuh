@@ -102,6 +102,16 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 
+// Steps of a page that is not there: the TMA fills its codes with zeros, the steps are plain copies, so the thread that would have copied them writes
+// zeros (what shared memory held could be NaN or huge).  Key steps at `to`, value steps `apart` bytes behind; in front of the thread's arrival.
+__device__ __forceinline__ void zero_steps(uint8_t* to, int apart, int rows) {
+    for (int i = 0; i < rows; i += 4) {
+        *reinterpret_cast<uint4*>(to + i * 4) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(to + apart + i * 4) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    ptx::fence_proxy_async_smem();                                      // (the slot's next steps come by asynchronous copies)
+}
+
 // A tile of 128 rows of D 16-bit channels as the tensor core wants it: lines of 64 channels, row r of line i at i * 16384 + r * 128, its 16-byte
 // chunk c at slot c ^ (r % 8).  A row of raw codes (as the TMA left them: chunks swizzled likewise) becomes a row of it.
 template <int D, typename T>

@@ -276,3 +276,38 @@ def test_queries_over_themselves():
         gpu, qd = pu.to_gpu(cache), q.cuda()
         want = vt.vitint_paged_attention(qd, gpu, batch, 0.09).clone()
         assert torch.equal(vt.vitint_paged_attention(qd, gpu, batch, 0.09, out=qd), want)
+
+
+# ---- data that the mask hides or the page table does not name ---------------------------------------------------------------------
+
+def _alternating(g, ctype, new, dim=128, places=16, group=1, count=400):
+    """Sequences of 41 tokens, whose last page ends in NaN, and between them ones of 60 whose third page is none of the cache's (the reference has a
+    page of zeros there): what a CTA had in shared memory before is NaN where the missing page's tokens lie."""
+    lengths = [41, 60] * (count // 2)
+    pages = sum(-(-n // places) for n in lengths) + 1
+    cache = pu.random_cache(g, pages, 2, places, dim, ctype)
+    table = pu.random_table(g, lengths, places, pages - 1)
+    pu.spoil_unused(cache, table, lengths)
+    with_zeros = vt.PagedCache(*(None if t is None else t.clone() for t in (cache.k, cache.v, cache.k_steps, cache.v_steps)))
+    for t in (with_zeros.k, with_zeros.v, with_zeros.k_steps, with_zeros.v_steps):
+        if t is not None:
+            t[pages - 1] = 0
+    bad, want = table.clone(), table.clone()
+    bad[1::2, 2] = torch.where(torch.arange(count // 2) % 2 == 0, -1, 1 << 30).to(torch.int32)
+    want[1::2, 2] = pages - 1
+    starts = (torch.arange(count + 1) * new).to(torch.int32)
+    q = torch.randn(count * new, 2 * group, dim, generator=g).to(F16 if ctype == F16 else BF16)
+    batch = vt.CacheBatch(bad.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 64)
+    return cache, with_zeros, want, lengths, starts, q, batch
+
+
+@pytest.mark.parametrize("window", [0, 10])
+@pytest.mark.parametrize("ctype", [BF16, F16, I8])
+@pytest.mark.parametrize("new", [1, 17])
+def test_missing_pages_are_zeros(new, ctype, window):
+    """Keys, values and steps of a page that is not there count as zeros, whatever shared memory held; behind a window they do not count."""
+    g = torch.Generator().manual_seed(60)
+    cache, with_zeros, table, lengths, starts, q, batch = _alternating(g, ctype, new, count=2400 if new == 1 else 400)      # several items a CTA
+    out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.09, window=window, want_lse=True)
+    assert vt.vitint_device_status() == -1
+    pu.check_attention(out, lse, pu.attention64(q, with_zeros, table, lengths, starts, 0.09, True, window))
