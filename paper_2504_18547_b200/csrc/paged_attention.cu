@@ -316,6 +316,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         }
         const int all_low = P.plan.window ? base + tokens - P.plan.window : 0;                               // the last row's
         const int all_high = P.plan.causal ? min(base + 1, w.s.length) : w.s.length;                         // the first row's
+        const int some_low = P.plan.window ? base - P.plan.window + 1 : 0;                                    // keys that some row sees
+        const int some_high = P.plan.causal ? min(base + tokens, w.s.length) : w.s.length;
         float o[D / 16][4 * NQ], m[NQ][2], l[NQ][2];
         uint32_t unit = 0x00800000u;                                     // CODES: the power of two that o is a multiple of
 #pragma unroll
@@ -432,7 +434,10 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             step[u][r] = vs[16 * u + 8 * r];
-                            if (edge && key0 + 16 * u + 8 * r + g >= w.s.length) step[u][r] = 0.0f;      // (behind the length: whatever lies there)
+                            if (edge) {                                  // no row sees it: whatever lies there, and no part of the largest step
+                                const int key = key0 + 16 * u + 8 * r + g;
+                                if (key < some_low || key >= some_high) step[u][r] = 0.0f;
+                            }
                             largest = max(largest, __float_as_uint(step[u][r]) & 0x7F800000u);
                         }
                     largest = min(__reduce_max_sync(0xffffffffu, largest), 0x7E000000u);

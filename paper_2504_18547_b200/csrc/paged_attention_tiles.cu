@@ -79,6 +79,7 @@ struct Half {
     int i0, rows;                                                       // first token (in the sequence's new ones), live rows
     int from, to;                                                       // tiles, from >= to: none
     int low_last, high_first;                                           // first key that the last token sees, end of what the first one sees
+    int low, high;                                                      // keys that some token sees
 };
 __device__ __forceinline__ Half half_of(const TilesParams& P, const StretchWalk<QueryRuns<PT_KEYS>>& w, int x) {
     Half h;
@@ -89,6 +90,8 @@ __device__ __forceinline__ Half half_of(const TilesParams& P, const StretchWalk<
     const int begin = P.plan.window ? max(base - P.plan.window + 1, 0) : 0;
     h.low_last = P.plan.window ? base + tokens - P.plan.window : 0;
     h.high_first = P.plan.causal ? min(base + 1, w.s.length) : w.s.length;
+    h.low = begin;
+    h.high = end;
     h.from = max(w.tile, (begin - w.first) / PT_KEYS);
     h.to = min(w.end, (end - w.first + PT_KEYS - 1) / PT_KEYS);
     if (tokens <= 0 || end <= begin) h.to = h.from;
@@ -446,7 +449,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const uint32_t word[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            if (key0 + 4 * lane + k < w.s.length) larger = max(larger, word[k] & 0x7F800000u);
+                            if (key0 + 4 * lane + k >= half.low && key0 + 4 * lane + k < half.high) larger = max(larger, word[k] & 0x7F800000u);
                         larger = min(__reduce_max_sync(0xffffffffu, larger), 0x7E000000u);
                     }
                     if (t == half.from) {

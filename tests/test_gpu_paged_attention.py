@@ -311,3 +311,20 @@ def test_missing_pages_are_zeros(new, ctype, window):
     out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.09, window=window, want_lse=True)
     assert vt.vitint_device_status() == -1
     pu.check_attention(out, lse, pu.attention64(q, with_zeros, table, lengths, starts, 0.09, True, window))
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_steps_of_hidden_tokens_do_not_count(new):
+    """Tokens in front of the window with steps 2^30 times as large: the others are taken relative to the largest step that some row sees."""
+    g = torch.Generator().manual_seed(61)
+    cache = pu.random_cache(g, 12, 2, 16, 128, I8)
+    table = pu.random_table(g, [120], 16, 12)
+    hidden = torch.arange(120 - new - 9)                                           # in front of the first new token's ten
+    seen_only = vt.PagedCache(cache.k, cache.v, cache.k_steps, cache.v_steps.clone())
+    cache.v_steps[table[0, hidden // 16].long(), :, hidden % 16] *= 2.0 ** 30
+    seen_only.v_steps[table[0, hidden // 16].long(), :, hidden % 16] = 0
+    q = torch.randn(new, 4, 128, generator=g).to(BF16)
+    starts = torch.tensor([0, new], dtype=torch.int32)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor([120], dtype=torch.int32).cuda(), starts.cuda(), new, 120)
+    out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.09, window=10, want_lse=True)
+    pu.check_attention(out, lse, pu.attention64(q, seen_only, table, [120], starts, 0.09, True, 10))
