@@ -47,6 +47,11 @@ struct RowsShape {
     static constexpr int SMEM = STAGES * (STAGE + 2 * STEPS) + MERGE + 256;
     static_assert(SMEM <= 233472 / CTAS - 1024, "shared memory");
 };
+// Operands' type of the second product, and the offset of the probabilities in it: they are at most 1.
+template <typename T, bool CODES>
+using RowsOperand = typename std::conditional<CODES, __half, T>::type;
+template <typename T, bool CODES>
+constexpr float ROWS_OFFSET = probability_offset<RowsOperand<T, CODES>>(0);
 
 struct RowsParams {
     PlanParams plan;
@@ -131,8 +136,9 @@ __device__ __forceinline__ void write_product(const RowsParams& P, const Sequenc
         __syncwarp();
     }
 }
+// (m is lower than the maximum that l refers to by the offset)
 template <int NQ>
-__device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s, int h, int p, const float (&m)[NQ][2], const float (&l)[NQ][2]) {
+__device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s, int h, int p, const float (&m)[NQ][2], const float (&l)[NQ][2], float offset) {
     const int lane = threadIdx.x & 31, i0 = p * P.plan.tile_tokens, rows = min(P.plan.tile_tokens, s.queries - i0) * P.plan.group;
     if (!P.lse || lane >= 4) return;
 #pragma unroll
@@ -142,7 +148,7 @@ __device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s
             const int row = 8 * n + 2 * lane + e;
             if (row >= rows) continue;
             const int i = row / P.plan.group, head = h * P.plan.group + row - i * P.plan.group;
-            P.lse[(long long)(s.first + i0 + i) * P.q_heads + head] = l[n][e] > 0.0f ? (m[n][e] + log2f(l[n][e])) * 0.69314718055994531f : -INFINITY;
+            P.lse[(long long)(s.first + i0 + i) * P.q_heads + head] = l[n][e] > 0.0f ? (m[n][e] + (log2f(l[n][e]) + offset)) * 0.69314718055994531f : -INFINITY;
         }
 }
 
@@ -157,7 +163,8 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // largest).  Probabilities times value steps enter the second contraction in fp16 too, relative to the largest step so far (its power of two), so
     // that they do not run out of exponents.
     constexpr bool RESCALED_Q = CODES && BF16;
-    using M = typename std::conditional<CODES, __half, T>::type;       // operands' type
+    using M = RowsOperand<T, CODES>;
+    constexpr float OFFSET = ROWS_OFFSET<T, CODES>;
     // A second product with what the first one's rounding left, except where the output is rounded eight times as coarsely, and where the
     // products would set the pace (two columns of products: 2 x 131,072 keys, twelve rows, 101 -> 121 us).
     constexpr bool SPLIT = NQ == 1 && !(CODES && BF16);
@@ -401,7 +408,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], x));
-                        from[n][e] = top[n][e] == -INFINITY ? 0.0f : top[n][e];
+                        from[n][e] = (top[n][e] == -INFINITY ? 0.0f : top[n][e]) - OFFSET;
                         grew = grew || top[n][e] != m[n][e];
                     }
                 if (__any_sync(0xffffffffu, grew)) {
@@ -409,7 +416,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float factor = exp2_approx(m[n][e] - from[n][e]);
+                            const float factor = exp2_approx((m[n][e] - OFFSET) - from[n][e]);
                             l[n][e] *= factor;
                             m[n][e] = top[n][e];
 #pragma unroll
@@ -440,7 +447,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                             }
                             largest = max(largest, __float_as_uint(step[u][r]) & 0x7F800000u);
                         }
-                    largest = min(__reduce_max_sync(0xffffffffu, largest), 0x7E000000u);
+                    largest = min(__reduce_max_sync(0xffffffffu, largest), 0x7E800000u);      // 2^126: its reciprocal is a normal number
                     if (largest != unit) {
                         const float down = __uint_as_float(0x3F800000u - min(largest - unit, 0x3F000000u));
 #pragma unroll
@@ -531,11 +538,20 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             advance();
         }
 
-        if (CODES) {
+        // o and l without the offset (exactly); m stays what the exponentials were taken relative to
+        if (CODES || OFFSET != 0.0f) {
+            const float back = (CODES ? __uint_as_float(unit) : 1.0f) * offset_back(OFFSET);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int e = 0; e < 4 * NQ; ++e) o[i][e] *= __uint_as_float(unit);
+                for (int e = 0; e < 4 * NQ; ++e) o[i][e] *= back;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    l[n][e] *= offset_back(OFFSET);
+                    m[n][e] -= OFFSET;
+                }
         }
         // ---- the four warps' results become one (every warp passes these barriers, whatever became of its waits) -------------
 #pragma unroll
@@ -594,7 +610,7 @@ paged_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     for (int e = 0; e < 2; ++e) inv[n][e] = l[n][e] > 0.0f ? 1.0f / l[n][e] : 0.0f;
 #pragma unroll
                 for (int mt = 0; mt < D / 16; ++mt) write_product<D, T, CODES, NQ>(P, w.s, w.h, w.p, mt, o[mt], inv);
-                write_lse<NQ>(P, w.s, w.h, w.p, m, l);
+                write_lse<NQ>(P, w.s, w.h, w.p, m, l, OFFSET);
             } else if (ok) {
                 put(P.partial + (2ll * blockIdx.x + (w.tile > 0 ? 0 : 1)) * S::PART);
             }
@@ -659,7 +675,7 @@ paged_rows_join_kernel(const __grid_constant__ RowsParams P) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) inv[n][e] = l[n][e] > 0.0f ? 1.0f / l[n][e] : 0.0f;
     write_product<D, T, CODES, NQ>(P, s, note.h, note.p, mt, o, inv);
-    if (mt == 0) write_lse<NQ>(P, s, note.h, note.p, m, l);
+    if (mt == 0) write_lse<NQ>(P, s, note.h, note.p, m, l, ROWS_OFFSET<T, CODES>);
 }
 
 inline int rows_grid(int nq) { return (nq == 1 ? 4 : 2) * sm_count(); }      // at most

@@ -40,6 +40,12 @@ struct TilesShape {
     static constexpr int PART = 2 * (D + 2) * 128;                      // floats of a partial result: [half][output columns, maximum, sum][row]
 };
 
+// Operands' type of the second product, and the offset of the probabilities in it: they are at most 2^8, as the maximum lags.
+template <typename T, bool CODES>
+using TilesOperand = typename std::conditional<CODES, __half, T>::type;
+template <typename T, bool CODES>
+constexpr float TILES_OFFSET = probability_offset<TilesOperand<T, CODES>>(8);
+
 struct TilesParams {
     PlanParams plan;                                                    // tile_tokens: of both halves
     int half_tokens;
@@ -156,7 +162,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr int LINES = S::LINES;
     // Codes: probabilities times value steps enter the second product in fp16, relative to the largest step so far (its power of two).
     constexpr bool SCALED = CODES;
-    using M = typename std::conditional<CODES, __half, T>::type;        // the second product's type
+    using M = TilesOperand<T, CODES>;
+    constexpr float OFFSET = TILES_OFFSET<T, CODES>;
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t O_COL = 256;                                     // tensor memory: S and P of the halves at 0 and 128, O at 256 and 256 + D
     extern __shared__ __align__(1024) uint8_t pt_smem[];
@@ -450,7 +457,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (key0 + 4 * lane + k >= half.low && key0 + 4 * lane + k < half.high) larger = max(larger, word[k] & 0x7F800000u);
-                        larger = min(__reduce_max_sync(0xffffffffu, larger), 0x7E000000u);
+                        larger = min(__reduce_max_sync(0xffffffffu, larger), 0x7E800000u);      // 2^126: its reciprocal is a normal number
                     }
                     if (t == half.from) {
                         m = mt;
@@ -460,7 +467,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const bool grow = mt > m + 8.0f;
                         if (__any_sync(0xffffffffu, grow) || larger != unit) {
                             const float now = grow ? mt : m;
-                            float factor = grow ? exp2_approx(m - now) : 1.0f;
+                            float factor = grow ? exp2_approx((m - OFFSET) - (now - OFFSET)) : 1.0f;
                             sum[0] = f2_mul(sum[0], f2_dup(factor));
                             sum[1] = f2_mul(sum[1], f2_dup(factor));
                             if (SCALED) factor *= __uint_as_float(0x3F800000u - min(larger - unit, 0x3F000000u));
@@ -480,7 +487,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             ptx::tmem_st_wait();
                         }
                     }
-                    const f32x2 minus_base = f2_dup(m == -INFINITY ? 0.0f : -m);
+                    const f32x2 minus_base = f2_dup(m == -INFINITY ? 0.0f : OFFSET - m);
                     const float up = SCALED ? __uint_as_float(0x7F000000u - unit) : 1.0f;
                     ptx::tmem_ld32(t_s, v[0]);
 #pragma unroll
@@ -516,7 +523,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             float a, b, c, d;
             f2_unpack(sum[0], a, b);
             f2_unpack(sum[1], c, d);
-            const float l = (a + b) + (c + d), scale = SCALED ? __uint_as_float(unit) : 1.0f;
+            // (o and l without the offset, exactly; the maximum is what the exponentials were taken relative to)
+            const float l = ((a + b) + (c + d)) * offset_back(OFFSET), scale = (SCALED ? __uint_as_float(unit) : 1.0f) * offset_back(OFFSET);
             const bool whole = w.whole();
             const long long token = w.s.first + half.i0 + i;
             const int head = w.h * P.plan.group + row - i * P.plan.group;
@@ -549,10 +557,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             if (live) {
                 if (!whole) {
-                    part[D * 128] = m;
+                    part[D * 128] = m - OFFSET;
                     part[(D + 1) * 128] = l;
                 } else if (P.lse) {
-                    P.lse[token * P.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+                    P.lse[token * P.q_heads + head] = l > 0.0f ? ((m - OFFSET) + (log2f(l) + OFFSET)) * 0.69314718055994531f : -INFINITY;
                 }
             }
             ptx::tc_fence_before();
@@ -568,7 +576,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // Joins the partial results of an item that several CTAs worked on.  Block (c, y): the item that began in front of CTA c + 1's stretch, half y / 4 of
 // it, a quarter of the output columns; a row a thread.
-template <int D, typename T>
+template <int D, typename T, bool CODES>
 __global__ void __launch_bounds__(128)
 paged_tiles_join_kernel(const __grid_constant__ TilesParams P) {
     constexpr int PART = 2 * (D + 2) * 128, COLS = D / 4;
@@ -616,7 +624,7 @@ paged_tiles_join_kernel(const __grid_constant__ TilesParams P) {
         for (int q = 0; q < 4; ++q) p[q] = pack16<T>(o[k + 2 * q] * inv, o[k + 2 * q + 1] * inv);
         *reinterpret_cast<uint4*>(to + k) = make_uint4(p[0], p[1], p[2], p[3]);
     }
-    if (P.lse && col0 == 0) P.lse[token * P.q_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (P.lse && col0 == 0) P.lse[token * P.q_heads + head] = l > 0.0f ? (m + (log2f(l) + TILES_OFFSET<T, CODES>)) * 0.69314718055994531f : -INFINITY;
 }
 
 inline size_t tiles_partial_bytes(int ctas, int head_dim) { return (size_t)ctas * 2 * 2 * (head_dim + 2) * 128 * 4; }
@@ -650,7 +658,7 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
     }
     launch_kernel(paged_tiles_kernel<D, T, CODES>, dim3(grid), dim3(S::THREADS), S::SMEM, st, map_q, map_k, map_v, P);
     if (int rc = cuda_status(cudaGetLastError())) return rc;
-    if (!P.plan.whole && grid > 1) launch_kernel(paged_tiles_join_kernel<D, T>, dim3(grid - 1, 8), dim3(128), 0, st, P);
+    if (!P.plan.whole && grid > 1) launch_kernel(paged_tiles_join_kernel<D, T, CODES>, dim3(grid - 1, 8), dim3(128), 0, st, P);
     return cuda_status(cudaGetLastError());
 }
 

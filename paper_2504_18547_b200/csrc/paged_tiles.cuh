@@ -102,6 +102,14 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 
+// fp16 holds 2^15 and more, but what lies below 2^-24 becomes 0: a probability enters the second product as the multiple 2^offset of itself, and so do
+// the sum that it is divided by and the maximum that both refer to (lower by the offset), so that the offset cancels.  Without it all that lies 17.4 nats
+// below the maximum would be lost from the output (not from the sum): behind one token, 131,072 of them at 17.5 nats hold 0.3 % of the weight.
+// `room`: how far above 1 a probability (times a step that is below 4 relative to the unit of the steps) may lie, as a power of two.
+template <typename M>
+__host__ __device__ constexpr float probability_offset(int room) { return std::is_same<M, __half>::value ? (float)(13 - room) : 0.0f; }
+__host__ __device__ constexpr float offset_back(float offset) { return 1.0f / (float)(1 << (int)offset); }
+
 // Steps of a page that is not there: the TMA fills its codes with zeros, the steps are plain copies, so the thread that would have copied them writes
 // zeros (what shared memory held could be NaN or huge).  Key steps at `to`, value steps `apart` bytes behind; in front of the thread's arrival.
 __device__ __forceinline__ void zero_steps(uint8_t* to, int apart, int rows) {

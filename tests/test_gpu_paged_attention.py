@@ -328,3 +328,38 @@ def test_steps_of_hidden_tokens_do_not_count(new):
     batch = vt.CacheBatch(table.cuda(), torch.tensor([120], dtype=torch.int32).cuda(), starts.cuda(), new, 120)
     out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.09, window=10, want_lse=True)
     pu.check_attention(out, lse, pu.attention64(q, seen_only, table, [120], starts, 0.09, True, 10))
+
+
+@pytest.mark.parametrize("qtype,ctype", [(F16, F16), (F16, I8), (BF16, I8)])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group,new,length", [(4, 1, 131073), (4, 1, 200), (4, 4, 9000), (4, 40, 9000), (1, 20, 300)])
+def test_a_tail_far_below_the_maximum_counts(group, new, length, dim, qtype, ctype):
+    """Every sixteenth token has the value 0 and, 17.5 nats below it, all others have 512: the output is 512 times the others' share of the sum.
+
+    A probability is off by half a step of the operand's type, 2^-11 relative, or where it is below fp16's normal range by half of 2^-24 over the
+    offset that it is taken with (2^5 at least), 2^-30 of the maximum; the output's rounding and the score's error (of size 17.5: products of d
+    channels and three roundings, (d + 8) 2^-24 17.5) come on top, and 2^-18 for ex2 and the sums."""
+    places = 128
+    pages = -(-length // places)
+    shape = (pages, 1, places, dim)
+    k, v = torch.zeros(shape), torch.full(shape, 512.0)
+    k[..., 0] = -1.0
+    k[:, 0, ::16, 0], v[:, 0, ::16] = 0.0, 0.0                                      # scores: 0, and -17.5 for all others
+    if ctype == I8:
+        cache = vt.PagedCache((k * 4).to(I8), (v / 256).to(I8), torch.full(shape[:3], 0.25), torch.full(shape[:3], 256.0))
+    else:
+        cache = vt.PagedCache(k.to(ctype), v.to(ctype))
+    q = torch.zeros(new, group, dim, dtype=qtype)
+    q[..., 0] = 17.5
+    batch = vt.CacheBatch(torch.arange(pages, dtype=torch.int32)[None].cuda(), torch.tensor([length], dtype=torch.int32).cuda(),
+                          torch.tensor([0, new], dtype=torch.int32).cuda(), new, length)
+    out, lse = vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 1.0, causal=False, want_lse=True)
+    top = -(-length // 16)
+    others = (length - top) * math.exp(-17.5)
+    want, half = 512 * others / (top + others), pu.EPS[qtype] / 2
+    relative = half + 2.0 ** -11 + 2 * (dim + 8) * 2.0 ** -24 * 17.5 + 2.0 ** -18
+    absolute = 512 * (length - top) / top * 2.0 ** -30 + (2.0 ** -25 if qtype == F16 else 0.0)       # (fp16 outputs' own subnormal step)
+    off = (out.double() - want).abs().max()
+    assert float(off) <= relative * want + absolute, (float(off), want)
+    z = math.log(top + others)
+    assert float((lse.double() - z).abs().max()) <= 2.0 ** -18 + 2.0 ** -22 * z
