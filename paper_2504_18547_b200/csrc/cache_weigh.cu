@@ -65,7 +65,7 @@ __device__ __forceinline__ void weigh_block(const uint32_t (&v)[32], const float
                 b = i + 2 * k + 1 >= low && i + 2 * k + 1 < high ? b : -INFINITY;
             }
             if (!MASKED && k == 1 && i % 16 != 12) {
-                exp2_poly(f2_pack(fmaxf(a, -126.0f), fmaxf(b, -126.0f)), a, b);
+                exp2_poly(f2_pack(max_or_nan(a, -127.0f), max_or_nan(b, -127.0f)), a, b);
             } else {
                 a = exp2_approx(a);
                 b = exp2_approx(b);

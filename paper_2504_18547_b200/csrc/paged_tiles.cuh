@@ -72,10 +72,17 @@ __device__ __forceinline__ uint2 codes_to_16x4(uint32_t four) {
     return make_uint2(codes_to_16<T>(__byte_perm(four, 0u, 0x4140)), codes_to_16<T>(__byte_perm(four, 0u, 0x4342)));
 }
 
-// 2^x of a pair, -126 <= x < 128, without the special-function unit: x = n + f with n the nearest integer (the constant 1.5 * 2^23 rounds), 2^f on
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// 2^x of a pair, -127 <= x < 128, without the special-function unit: x = n + f with n the nearest integer (the constant 1.5 * 2^23 rounds), 2^f on
 // [-1/2, 1/2] by a polynomial of degree five (weighted least squares on Chebyshev nodes until the relative error is even: 7.5e-8, 2.2e-7 with fp32
-// steps), n added to the exponent.  Eight packed operations and two integer ones take as long on the FMA pipe as the special-function unit takes for
-// two results, so a kernel that is bound by exponentials shares them between the two.
+// steps), times 2^n, which is 0 for n = -127.  What is no number stays none (an exponent added to the bits would make it finite).  Nine packed operations
+// and two integer ones take as long on the FMA pipe as the special-function unit takes for two results, so a kernel that is bound by exponentials
+// shares them between the two.
 __device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
     const f32x2 t = f2_add(x, f2_dup(12582912.0f));
     const f32x2 f = f2_fma(f2_add(t, f2_dup(-12582912.0f)), f2_dup(-1.0f), x);
@@ -86,9 +93,8 @@ __device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b) {
     p = f2_fma(p, f, f2_dup(1.000000119e+00f));
     float ta, tb;
     f2_unpack(t, ta, tb);
+    p = f2_mul(p, f2_pack(__uint_as_float((__float_as_uint(ta) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(tb) << 23) + 0x3F800000u)));
     f2_unpack(p, a, b);
-    a = __uint_as_float(__float_as_uint(a) + (__float_as_uint(ta) << 23));
-    b = __uint_as_float(__float_as_uint(b) + (__float_as_uint(tb) << 23));
 }
 
 // Bits of the columns of a block of 32 that a row sees: low <= column < high.

@@ -117,3 +117,38 @@ def test_same_bits_every_time_and_replay():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(w, first)
+
+
+@pytest.mark.parametrize("bad", [18, 22, 27, 31])
+@pytest.mark.parametrize("new", [3, 40])
+def test_queries_that_are_not_numbers_show(new, bad):
+    """A query row of NaN makes the weights of all tokens that it sees NaN, whichever column of the product it is; other heads' are as they were."""
+    g = torch.Generator().manual_seed(8)
+    cache = pu.random_cache(g, 20, 2, 16, 64, BF16)
+    table, lengths = pu.random_table(g, [300], 16, 20), [300]
+    starts, row = torch.tensor([0, new], dtype=torch.int32), bad % new
+    q = torch.randn(new, 2, 64, generator=g).to(BF16)
+    lse = pu.attention64(q, cache, table, lengths, starts, 0.1, True, 0)[1].float()
+    q[row, 1] = float("nan")
+    batch = vt.CacheBatch(table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 300)
+    w = vt.vitint_cache_weigh(q.cuda(), lse.cuda(), pu.to_gpu(cache), batch, 0.1, None, torch.zeros(20, 2, 16, device="cuda")).cpu()
+    j = torch.arange(300)
+    mine = w[table[0, j // 16].long(), :, j % 16]
+    seen = 300 - new + row + 1
+    assert bool(mine[:seen, 1].isnan().all()) and not bool(mine[seen:, 1].isnan().any()) and not bool(mine[:, 0].isnan().any())
+
+
+@pytest.mark.parametrize("new", [1, 120])
+def test_weights_too_small_for_their_type_are_zero(new):
+    """Tokens 200 nats below the rows' sums: their weight is below 2^-149, and 0 in every column of the product."""
+    g = torch.Generator().manual_seed(9)
+    cache = vt.PagedCache(torch.zeros(20, 1, 16, 64, dtype=BF16), torch.zeros(20, 1, 16, 64, dtype=BF16))
+    cache.k[:10, ..., 0] = -1.0
+    q = torch.zeros(new, 1, 64, dtype=BF16)
+    q[..., 0] = 200.0
+    batch = vt.CacheBatch(torch.arange(20, dtype=torch.int32)[None].cuda(), torch.tensor([320], dtype=torch.int32).cuda(),
+                          torch.tensor([0, new], dtype=torch.int32).cuda(), new, 320)
+    gpu = pu.to_gpu(cache)
+    _, lse = vt.vitint_paged_attention(q.cuda(), gpu, batch, 1.0, want_lse=True)
+    w = vt.vitint_cache_weigh(q.cuda(), lse, gpu, batch, 1.0, None, torch.full((20, 1, 16), 7.0, device="cuda"))
+    assert not bool(w[:10].any()) and bool((w[10:, 0, 0] > 0).all())
