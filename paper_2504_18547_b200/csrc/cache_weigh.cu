@@ -381,6 +381,9 @@ template <int D, typename T, bool CODES>
 int cache_weigh_launch(WeighParams& P, const void* q, int64_t tokens, int64_t q_token, int64_t q_head, const vitint_cache* cache,
                        const vitint_cache_batch* batch, void* workspace, cudaStream_t st) {
     constexpr int LINES = D / 64;
+    const long long runs = (batch->max_length + CW_KEYS - 1) / CW_KEYS, tiles = most_runs(batch, tokens, P.plan.tile_tokens);
+    long long items;
+    if (!plan_fits(cache, batch, runs, tiles, items)) return VITINT_ERR_UNSUPPORTED;
     const int box_tokens = P.plan.tile_tokens < batch->max_queries ? P.plan.tile_tokens : batch->max_queries;
     P.box_rows = box_tokens * P.plan.group;
     P.n_pad = (P.box_rows + 15) / 16 * 16;
@@ -400,9 +403,6 @@ int cache_weigh_launch(WeighParams& P, const void* q, int64_t tokens, int64_t q_
     if (!encode_query_map(&map_q, q, std::is_same<T, __nv_bfloat16>::value ? VITINT_BF16 : VITINT_F16, D, tokens, P.q_heads, q_token, q_head, P.plan.group, box_tokens) ||
         !encode_cache_map(&map_k, cache, cache->k, P.page_rows, CODES))
         return VITINT_ERR_CUDA;
-    const long long runs = (batch->max_length + CW_KEYS - 1) / CW_KEYS, tiles = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens;
-    const long long items = (long long)batch->sequences * cache->kv_heads * runs;
-    if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
     P.notes = (JoinNote*)workspace;
     P.partial = (float*)((uint8_t*)workspace + notes_bytes(weigh_grid()));
     return few ? cache_weigh_go<D, T, CODES, true>(P, map_q, map_k, smem, items * tiles, st) : cache_weigh_go<D, T, CODES, false>(P, map_q, map_k, smem, items * tiles, st);

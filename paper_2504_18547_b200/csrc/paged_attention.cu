@@ -686,10 +686,10 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     using S = RowsShape<D, CODES, NQ>;
     CUtensorMap map_k, map_v;
     P.page_rows = cache->page_tokens < S::KT ? cache->page_tokens : S::KT;
+    const long long tiles = (batch->max_length + S::KT - 1) / S::KT;
+    long long items;
+    if (!plan_fits(cache, batch, most_runs(batch, P.plan.seq.tokens, P.plan.tile_tokens), tiles, items)) return VITINT_ERR_UNSUPPORTED;
     if (!encode_cache_map(&map_k, cache, cache->k, P.page_rows, true) || !encode_cache_map(&map_v, cache, cache->v, P.page_rows, true)) return VITINT_ERR_CUDA;
-    const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + S::KT - 1) / S::KT;
-    const long long items = (long long)batch->sequences * cache->kv_heads * runs;
-    if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
     P.plan.whole = tiles <= WHOLE_TILES_ROWS;
     int grid = S::CTAS * sm_count();
     if (grid > items * tiles) grid = (int)(items * tiles);

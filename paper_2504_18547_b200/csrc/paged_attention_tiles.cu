@@ -634,6 +634,9 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
                        void* workspace, cudaStream_t st) {
     using S = TilesShape<D, CODES>;
     static_assert(S::SMEM <= 227 * 1024 && S::SLOTS <= PT_MAX_SLOTS && S::RAW_SLOTS <= 4, "shared memory");
+    const long long tiles = (batch->max_length + PT_KEYS - 1) / PT_KEYS;
+    long long items;
+    if (!plan_fits(cache, batch, most_runs(batch, tokens, P.plan.tile_tokens), tiles, items)) return VITINT_ERR_UNSUPPORTED;
     const int box_tokens = P.half_tokens < batch->max_queries ? P.half_tokens : batch->max_queries;
     P.box_rows = box_tokens * P.plan.group;
     P.page_rows = cache->page_tokens;
@@ -641,9 +644,6 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
     if (!encode_query_map(&map_q, q, std::is_same<T, __nv_bfloat16>::value ? VITINT_BF16 : VITINT_F16, D, tokens, P.q_heads, q_token, q_head, P.plan.group, box_tokens) ||
         !encode_cache_map(&map_k, cache, cache->k, P.page_rows, CODES) || !encode_cache_map(&map_v, cache, cache->v, P.page_rows, CODES))
         return VITINT_ERR_CUDA;
-    const long long runs = (batch->max_queries + P.plan.tile_tokens - 1) / P.plan.tile_tokens, tiles = (batch->max_length + PT_KEYS - 1) / PT_KEYS;
-    const long long items = (long long)batch->sequences * cache->kv_heads * runs;
-    if (items > 0x7fffffffll || items * tiles > 0x7fffffffll) return VITINT_ERR_UNSUPPORTED;
     P.plan.whole = tiles <= WHOLE_TILES_CHUNKS;
     int grid = sm_count();
     if (grid > items * tiles) grid = (int)(items * tiles);

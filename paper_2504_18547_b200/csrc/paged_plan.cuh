@@ -110,7 +110,7 @@ template <typename Runs>
 __device__ __forceinline__ Stretch plan_stretch(const PlanParams& A, int cta, int ctas, bool& bad) {
     const int lane = threadIdx.x & 31;
     bool ok = true;
-    int total = 0;                                                     // (the host has checked that all tiles together fit)
+    int total = 0;                                                     // (plan_fits)
     const int first32 = sequence_tiles<Runs>(A, lane, ok);               // kept: most calls have no more sequences
     {
         int sum = first32;
@@ -253,6 +253,19 @@ inline PlanParams plan_params(const vitint_cache* cache, const vitint_cache_batc
     a.causal = causal;
     a.window = window >= batch->max_length ? 0 : window;
     return a;
+}
+
+// Items (heads of the cache times a sequence's runs) and all their tiles, for the host's bounds.  The device counts tiles in 32 bits, and rounds their number
+// up to the CTAs' stretches: false where that does not hold them.
+constexpr long long PLAN_MOST_TILES = 0x7fffffffll - (1 << 16);
+inline bool plan_fits(const vitint_cache* cache, const vitint_cache_batch* batch, long long runs, long long tiles, long long& items) {
+    items = (long long)batch->sequences * cache->kv_heads * runs;        // (each below 2^16, 2^16 and 2^25)
+    return items <= PLAN_MOST_TILES && items * tiles <= PLAN_MOST_TILES;
+}
+// Runs of `tokens` new tokens each that a sequence may have: no more new tokens than the call has rows, whatever the host's bound.
+inline long long most_runs(const vitint_cache_batch* batch, int64_t rows, int tokens) {
+    const int64_t most = batch->max_queries < rows ? batch->max_queries : rows;
+    return (most + tokens - 1) / tokens;
 }
 
 inline size_t notes_bytes(int ctas) { return ((size_t)ctas * sizeof(JoinNote) + 255) & ~(size_t)255; }

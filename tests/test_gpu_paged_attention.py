@@ -363,3 +363,17 @@ def test_a_tail_far_below_the_maximum_counts(group, new, length, dim, qtype, cty
     assert float(off) <= relative * want + absolute, (float(off), want)
     z = math.log(top + others)
     assert float((lse.double() - z).abs().max()) <= 2.0 ** -18 + 2.0 ** -22 * z
+
+
+def test_any_bound_of_the_new_tokens():
+    """max_queries may be as large as its type holds: no sequence has more new tokens than there are rows."""
+    g = torch.Generator().manual_seed(62)
+    cache, table, lengths, starts, q, batch = _small(g, ((90, 30), (200, 77)))
+    gpu, qd = pu.to_gpu(cache), q.cuda()
+    want, lse = vt.vitint_paged_attention(qd, gpu, batch, 0.09, want_lse=True)
+    loose = vt.CacheBatch(batch.page_table, batch.lengths, batch.query_starts, 2 ** 31 - 1, batch.max_length)
+    assert torch.equal(vt.vitint_paged_attention(qd, gpu, loose, 0.09), want)
+    places = (cache.k.shape[0], cache.k.shape[1], cache.k.shape[2])
+    first = vt.vitint_cache_weigh(qd, lse, gpu, batch, 0.09, None, torch.zeros(places, device="cuda"))
+    assert torch.equal(vt.vitint_cache_weigh(qd, lse, gpu, loose, 0.09, None, torch.zeros(places, device="cuda")), first)
+    assert vt.vitint_device_status() == 0

@@ -151,3 +151,17 @@ def test_the_binding_checks_its_tensors(B, monkeypatch):
                  slots=torch.zeros(3, dtype=torch.int64)) | change
         with pytest.raises(B.VitintError):
             B.vitint_qk_norm_rotate(**f)
+
+
+@pytest.mark.parametrize("change", [
+    dict(sequences=18705, max_length=57404 * 64, stride=1 << 20),                       # 2 heads x 57,404 tiles of 64: 2^31 - 8 tiles
+    dict(sequences=65535, max_length=1 << 24, stride=1 << 20),
+    dict(sequences=65535, max_length=1 << 24, stride=1 << 20, max_queries=2 ** 31 - 1)])
+def test_more_tiles_than_the_plan_counts(B, change):
+    """The plan rounds up to the CTAs' stretches in 32 bits: calls that come near 2^31 tiles are refused before anything else is done with them."""
+    work = dict(workspace=FAKE, size=1 << 40)
+    assert attention(B, b=batch(B, **change), tokens=(1 << 24) - 1, **work) == UNSUPPORTED
+    weigh = lambda **c: B.lib().vitint_cache_weigh(FAKE, BF16, (1 << 24) - 1, 8, 1024, 128, FAKE, cache(B), batch(B, **c), 0.1, 1, 0, None, FAKE, FAKE, 1 << 40, None)
+    if change["sequences"] == 65535:
+        assert weigh(**change) == UNSUPPORTED
+    assert weigh(**change | dict(max_length=14351 * 256, max_queries=4 * 32)) == UNSUPPORTED            # 4 runs of queries: the same number
