@@ -99,7 +99,8 @@ int vitint_version(void);
 
 /* Reads (and clears) the device status word of the current device; synchronizes
  * the device.  Returns VITINT_OK, VITINT_ERR_TIMEOUT, VITINT_ERR_INVALID_ARG (a kernel met data that contradicts what
- * its caller declared: vitint_softmax_quantize_bounded) or VITINT_ERR_CUDA. */
+ * its caller declared: vitint_softmax_quantize_bounded and the operators of the paged cache) or VITINT_ERR_CUDA.  The paged
+ * cache has a word of its own, which is read where the first one holds nothing: where both do, two calls return them. */
 int vitint_device_status(void);
 
 /* Self-test of the bounded wait: launches one warp that waits on a barrier nothing ever completes, with a limit of

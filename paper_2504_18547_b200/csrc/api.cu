@@ -62,6 +62,6 @@ extern "C" int64_t vitint_packed_pitch(int64_t cols, int32_t bits) {
 
 extern "C" int vitint_device_status(void) {
     if (cudaDeviceSynchronize() != cudaSuccess) return VITINT_ERR_CUDA;
-    const int h = take_status_word(), c = take_cache_status_word();
-    return h != 0 ? h : c;
+    const int h = take_status_word();
+    return h != 0 ? h : take_cache_status_word();       // (what the other word says waits for the next call)
 }

@@ -1,6 +1,7 @@
 // The paged cache: host checks of its descriptors, and what its kernels share on the device.
 #pragma once
 
+#include <atomic>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -116,7 +117,11 @@ struct SequenceView {
 
 inline int page_shift_of(const vitint_cache* c) { return c->page_tokens == 16 ? 4 : c->page_tokens == 32 ? 5 : c->page_tokens == 64 ? 6 : 7; }
 
+// Whether a kernel of this unit may have written its status word: those that do so take sequences.
+static std::atomic<bool> g_cache_called{false};
+
 inline SequenceView sequence_view(const vitint_cache* c, const vitint_cache_batch* b, int64_t tokens) {
+    g_cache_called.store(true, std::memory_order_relaxed);
     SequenceView s{};
     s.page_table = b->page_table; s.lengths = b->lengths; s.starts = b->query_starts;
     s.table_stride = b->table_stride;

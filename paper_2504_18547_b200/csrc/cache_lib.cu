@@ -4,4 +4,4 @@
 #include "paged_attention.cu"
 #include "cache_weigh.cu"
 
-int vitint::take_cache_status_word() { return take_status_word(); }
+int vitint::take_cache_status_word() { return g_cache_called.load(std::memory_order_relaxed) ? take_status_word() : VITINT_OK; }

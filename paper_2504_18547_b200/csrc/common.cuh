@@ -27,7 +27,7 @@ static inline int take_status_word() {
     }
     return h;
 }
-int take_cache_status_word();          // that of cache_lib.cu
+int take_cache_status_word();          // that of cache_lib.cu; no copy where none of its operators that report has been called
 
 inline int container_bits(int bits) { return bits == 3 ? 4 : bits; }
 inline bool valid_bits(int bits) { return bits == 2 || bits == 3 || bits == 4 || bits == 8; }

@@ -377,3 +377,14 @@ def test_any_bound_of_the_new_tokens():
     first = vt.vitint_cache_weigh(qd, lse, gpu, batch, 0.09, None, torch.zeros(places, device="cuda"))
     assert torch.equal(vt.vitint_cache_weigh(qd, lse, gpu, loose, 0.09, None, torch.zeros(places, device="cuda")), first)
     assert vt.vitint_device_status() == 0
+
+
+def test_the_status_keeps_what_it_has_not_reported():
+    """A wait that gave up and a page index outside the cache, both before the status is asked for: two answers, one after the other."""
+    g = torch.Generator().manual_seed(63)
+    cache, table, lengths, starts, q, batch = _small(g)
+    batch.page_table[0, 0] = -1
+    vt.vitint_paged_attention(q.cuda(), pu.to_gpu(cache), batch, 0.09)
+    vt.vitint_selftest_wait_timeout(1000000)
+    assert sorted(vt.vitint_device_status() for _ in range(3)) == [-7, -1, 0]
+    assert vt.vitint_device_status() == 0
