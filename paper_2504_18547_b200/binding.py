@@ -689,10 +689,13 @@ class PagedCache:
         device = _cuda_device() if device is None else device
         shape, stride, dtype = k.shape, k.stride(), k.dtype
         kind = _DTYPES.get(dtype, DTYPE_F32)
-        if (kind == DTYPE_F32 or len(shape) != 4 or v.dtype is not dtype or v.shape != shape or v.stride() != stride or stride[3] != 1
-                or k.get_device() != device or v.get_device() != device):
+        if (kind == DTYPE_F32 or len(shape) != 4 or v.dtype is not dtype or v.shape != shape or stride[3] != 1 or k.get_device() != device
+                or v.get_device() != device or v.stride() != stride and any(n > 1 and a != b for n, a, b in zip(shape, stride, v.stride()))):
             _require(False, where, "k and v have one type (bf16, fp16, int8), shape and strides, channels last, and are on the current device")
         pages, heads, places, dim = shape
+        # one page's or head's stride is nothing that is stepped by
+        page_stride = stride[0] if pages > 1 else heads * places * dim
+        head_stride = stride[1] if heads > 1 else places * dim
         if kind == DTYPE_I8:
             _require(ks is not None and vs is not None, where, "codes come with steps")
             steps = (_array(ks, torch.float32, pages * heads * places, device, where, "k_steps"),
@@ -700,7 +703,7 @@ class PagedCache:
         else:
             _require(ks is None and vs is None, where, "16-bit values have no steps")
             steps = (0, 0)
-        return _PACK_CACHE(k.data_ptr(), v.data_ptr(), *steps, pages, stride[0], stride[1], stride[2], heads, places, dim, kind)
+        return _PACK_CACHE(k.data_ptr(), v.data_ptr(), *steps, pages, page_stride, head_stride, stride[2], heads, places, dim, kind)
 
 
 @dataclass
@@ -763,14 +766,14 @@ def vitint_qk_norm_rotate(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tens
         stride = t.stride()
         if t.dtype is not dtype or t.shape != (tokens, width) or stride[1] != 1 or width % head_dim or t.get_device() != device:
             _require(False, where, "q, k and v are rows [tokens, heads * head_dim] of one type on the current device")
-        return t.data_ptr(), stride[0] if tokens > 1 else max(stride[0], width)
+        return t.data_ptr(), stride[0] if tokens > 1 else width       # (a single row's stride is nothing that is stepped by)
 
     def heads(t, n):
         """(address, stride) of output rows."""
         stride = t.stride()
         if t.dtype is not out_dtype or t.shape != (tokens, n, head_dim) or stride[2] != 1 or (n > 1 and stride[1] != head_dim) or t.get_device() != device:
             _require(False, where, "q_out and k_out are [tokens, heads, head_dim] of one 16-bit type, heads behind one another")
-        return t.data_ptr(), stride[0] if tokens > 1 else max(stride[0], n * head_dim)
+        return t.data_ptr(), stride[0] if tokens > 1 else n * head_dim
 
     if out_dtype is None:
         out_dtype = (q_out.dtype if q_out is not None else k_out.dtype if k_out is not None else
@@ -824,7 +827,7 @@ def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, where: str, 
         _require(False, where, "q is [tokens, q_heads, head_dim], channels last, on the current device")
     _require(batch.query_starts is not None, where, "the batch names the queries' rows")
     # a single token's or head's stride is nothing that is stepped by
-    head = stride[1] if shape[1] > 1 else max(stride[1], shape[2])
+    head = stride[1] if shape[1] > 1 else shape[2]
     return (shape[0], shape[1], _DTYPES.get(q.dtype, DTYPE_F32), stride[0] if shape[0] > 1 else shape[1] * head, head, cache.desc(where, device),
             batch.desc(where, device, kv[2]))
 
@@ -847,7 +850,7 @@ def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch
     elif out.shape != q.shape or out.dtype is not q.dtype or out.stride(2) != 1 or out.get_device() != device:
         _require(False, where, "out has the shape and type of q, channels last, and is on the current device")
     stride = out.stride()
-    out_head = stride[1] if heads > 1 else max(stride[1], out.shape[2])
+    out_head = stride[1] if heads > 1 else out.shape[2]
     if lse is not None:
         lse_at = _array(lse, torch.float32, tokens * heads, device, where, "lse")
     elif want_lse:

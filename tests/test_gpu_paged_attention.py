@@ -388,3 +388,23 @@ def test_the_status_keeps_what_it_has_not_reported():
     vt.vitint_selftest_wait_timeout(1000000)
     assert sorted(vt.vitint_device_status() for _ in range(3)) == [-7, -1, 0]
     assert vt.vitint_device_status() == 0
+
+
+def test_strides_that_nothing_steps_by():
+    """One query row, one head, one page: what their strides are does not matter, and keys' and values' need not agree there."""
+    g = torch.Generator().manual_seed(64)
+    d, places = 64, 16
+    cache = pu.random_cache(g, 1, 1, places, d, BF16)
+    table, lengths = torch.zeros(1, 1, dtype=torch.int32), [13]
+    loose = lambda t, page, head: torch.empty(8192, dtype=t.dtype, device="cuda").as_strided(t.shape, (page, head, d, 1)).copy_(t)
+    one_page = vt.PagedCache(loose(cache.k, 1031, 1), loose(cache.v, 17, 1025))
+    for new, heads in ((1, 1), (1, 3), (5, 1), (13, 2), (3, 1)):
+        q = torch.randn(new, heads, d, generator=g).to(BF16)
+        strides = (2 * d * heads + 8 if new > 1 else 77, d if heads > 1 else 3, 1)
+        qd, out = (torch.zeros(8192, dtype=BF16, device="cuda").as_strided(q.shape, strides) for _ in range(2))
+        qd.copy_(q)
+        starts = torch.tensor([0, new], dtype=torch.int32)
+        batch = vt.CacheBatch(table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 13)
+        _, lse = vt.vitint_paged_attention(qd, one_page, batch, 0.09, out=out, want_lse=True)
+        pu.check_attention(out, lse, pu.attention64(q, cache, table, lengths, starts, 0.09, True, 0))
+    assert vt.vitint_device_status() == 0

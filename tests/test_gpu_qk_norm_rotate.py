@@ -170,3 +170,21 @@ def test_other_stream_and_replay():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(q_out, want) and torch.equal(cache.k[0, 0, 8:], want_k[0, 0, :8])
+
+
+def test_one_token_of_rows_of_any_width():
+    """A single row's stride is nothing that is stepped by: here 388 elements, no multiple of 16 bytes, and other outputs' likewise."""
+    g = torch.Generator().manual_seed(7)
+    rows = torch.randn(3, 388, generator=g).to(BF16).cuda()
+    row = rows[2:3]                                                                    # (1552 bytes in: aligned)
+    outs = [torch.zeros(1, 260, dtype=BF16, device="cuda").as_strided((1, n, 128), (131, 128, 1)) for n in (1, 1)]
+    one = torch.ones(128, device="cuda")
+    make = lambda: vt.PagedCache.empty(1, 1, 16, 128)
+    given, plain = make(), make()
+    for cache in (given, plain):
+        cache.k.zero_(), cache.v.zero_()
+    slot = torch.tensor([5], device="cuda")
+    q, k = vt.vitint_qk_norm_rotate(row[:, :128], row[:, 128:256], row[:, 256:384], 128, q_gain=one, k_gain=one, q_out=outs[0], k_out=outs[1], cache=given, slots=slot)
+    parts = [row[:, i:i + 128].contiguous() for i in (0, 128, 256)]
+    q2, _ = vt.vitint_qk_norm_rotate(*parts, 128, q_gain=one, k_gain=one, cache=plain, slots=slot)
+    assert torch.equal(q, q2) and torch.equal(k[0, 0], plain.k[0, 0, 5]) and torch.equal(given.k, plain.k) and torch.equal(given.v, plain.v)
