@@ -758,6 +758,8 @@ def vitint_qk_norm_rotate(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tens
         _require(False, where, "rows are fp32, bf16 or fp16, the norm is none, rms or layer")
     if (v is None) is not (cache is None) or (slots is None) is not (cache is None):
         _require(False, where, "v and slots come with a cache")
+    if len(k.shape) != 2 or q is not None and len(q.shape) != 2 or not 0 < head_dim < 1 << 31:
+        _require(False, where, "q, k and v are rows [tokens, heads * head_dim] of one type on the current device")
     tokens, k_width = k.shape
     hk = k_width // head_dim
 
@@ -820,12 +822,13 @@ def _workspace(t: torch.Tensor, device: int, where: str) -> int:
     return t.nbytes
 
 
-def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, where: str, device: int):
+def _queries(q: torch.Tensor, cache: PagedCache, batch: CacheBatch, window: int, where: str, device: int):
     """(tokens, heads, type, strides, descriptors) of a call's queries, cache and batch."""
     shape, stride, kv = q.shape, q.stride(), cache.k.shape
-    if len(shape) != 3 or shape[2] != kv[-1] or stride[2] != 1 or q.get_device() != device:
-        _require(False, where, "q is [tokens, q_heads, head_dim], channels last, on the current device")
-    _require(batch.query_starts is not None, where, "the batch names the queries' rows")
+    if len(shape) != 3 or len(kv) != 4 or shape[2] != kv[3] or stride[2] != 1 or q.get_device() != device:
+        _require(False, where, "q is [tokens, q_heads, head_dim] of the cache's head_dim, channels last, on the current device")
+    if batch.query_starts is None or not 0 <= window < 1 << 31:
+        _require(False, where, "the batch names the queries' rows, and the window is a count of tokens")
     # a single token's or head's stride is nothing that is stepped by
     head = stride[1] if shape[1] > 1 else shape[2]
     return (shape[0], shape[1], _DTYPES.get(q.dtype, DTYPE_F32), stride[0] if shape[0] > 1 else shape[1] * head, head, cache.desc(where, device),
@@ -843,7 +846,7 @@ def vitint_paged_attention(q: torch.Tensor, cache: PagedCache, batch: CacheBatch
     out, or (out, lse [tokens, q_heads]) where lse is given or wanted."""
     where = "vitint_paged_attention"
     device = _cuda_device()
-    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, where, device)
+    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, window, where, device)
     L = lib()
     if out is None:
         out = torch.empty_like(q)
@@ -881,7 +884,7 @@ def vitint_cache_weigh(q: torch.Tensor, lse: torch.Tensor, cache: PagedCache, ba
     vitint_paged_attention returned for them) to weights_in [pages, kv_heads, page_tokens] (None: to zero).  Returns weights_out."""
     where = "vitint_cache_weigh"
     device, f32 = _cuda_device(), torch.float32
-    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, where, device)
+    tokens, heads, kind, q_token, q_head, dc, db = _queries(q, cache, batch, window, where, device)
     L = lib()
     places = cache.k.numel() // q.shape[2]
     if workspace is None:
@@ -903,8 +906,10 @@ def vitint_cache_evict(cache: PagedCache, batch: CacheBatch, weights: torch.Tens
     and copies them to the pages of new_table.  Returns (kept [sequences, kv_heads, budget], counts [sequences])."""
     where = "vitint_cache_evict"
     device, i32 = _cuda_device(), torch.int32
+    _require(len(cache.k.shape) == 4, where, "k and v are [pages, kv_heads, page_tokens, head_dim]")
     n, (_, heads, places, dim) = batch.lengths.numel(), cache.k.shape
-    _require(0 < budget < 1 << 31, where, "a budget of at least one token")
+    _require(0 < budget < 1 << 31 and 0 <= sinks <= budget and 0 <= recent <= budget - sinks, where,
+             "a budget of at least one token, first and last ones among them")
     if kept is None:
         kept = weights.new_empty((n, heads, budget), dtype=i32)
     if counts is None:

@@ -165,3 +165,35 @@ def test_more_tiles_than_the_plan_counts(B, change):
     if change["sequences"] == 65535:
         assert weigh(**change) == UNSUPPORTED
     assert weigh(**change | dict(max_length=14351 * 256, max_queries=4 * 32)) == UNSUPPORTED            # 4 runs of queries: the same number
+
+
+def test_the_binding_refuses_what_its_types_do_not_hold(B, monkeypatch):
+    """Counts beyond 32 bits (which would be cut to something else), and tensors of other orders: the library's error, not a wrong call or another error."""
+    monkeypatch.setattr(B, "_cuda_device", lambda: -1)                                  # the CPU: every call below is refused before the library is entered
+    monkeypatch.setattr(B, "_stream", lambda: 0)
+    text = B.lib().vitint_status_string
+
+    class Closed:
+        def __getattr__(self, name):
+            return text if name == "vitint_status_string" else pytest.fail(f"{name} was entered")
+
+    monkeypatch.setattr(B, "lib", Closed)
+    c = B.PagedCache(torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16))
+    flat = B.PagedCache(torch.zeros(4, 32, 64, dtype=torch.bfloat16), torch.zeros(4, 32, 64, dtype=torch.bfloat16))
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    b = B.CacheBatch(i32(2, 4), i32(2), i32(3), 1, 64)
+    q, weights, lse, rows = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 16), torch.zeros(2, 4), torch.zeros(3, 128, dtype=torch.bfloat16)
+    for window in (1 << 31, (1 << 32) + 5, -1, -(1 << 32)):
+        with pytest.raises(B.VitintError):
+            B.vitint_paged_attention(q, c, b, 0.1, window=window)
+        with pytest.raises(B.VitintError):
+            B.vitint_cache_weigh(q, lse, c, b, 0.1, None, weights, window=window)
+    for change in (dict(sinks=1 << 32), dict(recent=(1 << 32) + 1), dict(sinks=-1), dict(recent=-(1 << 32))):
+        with pytest.raises(B.VitintError):
+            B.vitint_cache_evict(c, b, weights, 4, i32(2, 2), **change)
+    for call in (lambda: B.vitint_paged_attention(q, flat, b, 0.1), lambda: B.vitint_cache_weigh(q, lse, flat, b, 0.1, None, weights),
+                 lambda: B.vitint_cache_evict(flat, b, weights, 4, i32(2, 2)), lambda: B.vitint_qk_norm_rotate(rows, rows[0], rows, 64, norm="none"),
+                 lambda: B.vitint_qk_norm_rotate(rows[0], rows, None, 64, norm="none"), lambda: B.vitint_qk_norm_rotate(rows, rows, None, 0, norm="none"),
+                 lambda: B.vitint_qk_norm_rotate(rows, rows, None, -64, norm="none"), lambda: B.vitint_qk_norm_rotate(rows, rows, None, 1 << 40, norm="none")):
+        with pytest.raises(B.VitintError):
+            call()
