@@ -690,8 +690,8 @@ int paged_rows_launch(RowsParams& P, const vitint_cache* cache, const vitint_cac
     long long items;
     if (!plan_fits(cache, batch, most_runs(batch, P.plan.seq.tokens, P.plan.tile_tokens), tiles, items)) return VITINT_ERR_UNSUPPORTED;
     if (!encode_cache_map(&map_k, cache, cache->k, P.page_rows, true) || !encode_cache_map(&map_v, cache, cache->v, P.page_rows, true)) return VITINT_ERR_CUDA;
-    P.plan.whole = tiles <= WHOLE_TILES_ROWS;
     int grid = S::CTAS * sm_count();
+    P.plan.whole = whole_items(items, tiles, grid, NQ == 1 ? 3 : 1, 8);
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
     P.partial = (float*)((uint8_t*)workspace + notes_bytes(rows_grid(NQ)));

@@ -644,8 +644,8 @@ int paged_tiles_launch(TilesParams& P, const void* q, int64_t tokens, int64_t q_
     if (!encode_query_map(&map_q, q, std::is_same<T, __nv_bfloat16>::value ? VITINT_BF16 : VITINT_F16, D, tokens, P.q_heads, q_token, q_head, P.plan.group, box_tokens) ||
         !encode_cache_map(&map_k, cache, cache->k, P.page_rows, CODES) || !encode_cache_map(&map_v, cache, cache->v, P.page_rows, CODES))
         return VITINT_ERR_CUDA;
-    P.plan.whole = tiles <= WHOLE_TILES_CHUNKS;
     int grid = sm_count();
+    P.plan.whole = whole_items(items, tiles, grid, 3, 4);
     if (grid > items * tiles) grid = (int)(items * tiles);
     P.notes = (JoinNote*)workspace;
     P.partial = (float*)((uint8_t*)workspace + notes_bytes(sm_count()));

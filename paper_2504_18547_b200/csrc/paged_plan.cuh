@@ -1,10 +1,11 @@
 // How the attention kernels over the paged cache share their work out.
 //
 // An item is, for the attention, a head of the cache and a run of a sequence's new tokens (tile_tokens of them, all query heads of the
-// group); its work is a number of key tiles.  (For the weighing it is a run of keys, and its work the runs of queries.)  All items' tiles, sequence by sequence, head by head, run by run, form one line, and every CTA
-// takes an equal stretch of it: whatever the lengths are, no CTA has more than one tile above the mean.  A stretch that ends inside
-// an item leaves a partial result (row maxima, sums and unnormalised outputs) in the workspace, at most two a CTA, and a second
-// kernel joins them.  The plan is made on the device from the lengths, so a recorded graph may be replayed with others; it is a
+// group); its work is a number of key tiles.  (For the weighing it is a run of keys, and its work the runs of queries.)  All items' tiles,
+// sequence by sequence, head by head, run by run, form one line, and every CTA takes an equal stretch of it: whatever the lengths are, no CTA
+// has more than one tile above the mean.  A stretch that ends inside an item leaves a partial result (row maxima, sums and unnormalised outputs)
+// in the workspace, at most two a CTA, and a second kernel joins them.  Short items stay whole (whole_items): a CTA then has all tiles of the items
+// that begin in its stretch, up to an item's less one above its share.  The plan is made on the device from the lengths, so a recorded graph may be replayed with others; it is a
 // warp's work: lanes take sequences, or the runs of one long chunk.
 #pragma once
 
@@ -19,10 +20,15 @@ struct PlanParams {
     int whole;                            // items are not split: a CTA has those that begin in its stretch
 };
 
-// Where the longest item is this short, splitting gains less than the second launch costs, whose host time sets the pace of small calls: a call after
-// another of one token over 777 cached ones (12 heads of 64, 7 tiles) takes 18.7 instead of 21.3 us, though 10.6 instead of 7.8 on the device; with more
-// items the device gains too (16 sequences of up to 300 tokens, 32/8 heads of 128: 10.2 instead of 11.8; 4 chunks of up to 300: 26.5 instead of 29.8).
-constexpr long long WHOLE_TILES_ROWS = 8, WHOLE_TILES_CHUNKS = 4;
+// Whether items stay whole: a second launch to join parts costs about 1.5 us on the device (and 2.2 us of the host).  That is more than what splitting gains where
+// the longest item has at most `few` tiles, and up to `most` tiles where the items alone fill a quarter of the grid.  Recorded calls, us whole / split:
+//   one token, 12 heads of 64, tiles of 128 keys, one sequence:  3 tiles 7.1 / 7.4,  4: 7.9 / 7.5,  7: 10.1 / 7.4;  16 sequences:  4: 9.2 / 10.6,  7: 12.3 / 13.2;
+//   one token, 32/8 heads of 128, tiles of 64:  one sequence  3: 7.4 / 7.7,  6: 9.1 / 7.7;  8 sequences  6: 10.2 / 9.9;  16 sequences  6: 11.0 / 11.2;
+//   the same over codes (a grid a third larger):  one sequence  2: 7.7 / 8.2,  4: 9.5 / 8.4;  16 sequences  4: 12.4 / 11.4,  8: 18.0 / 13.2;  64 sequences  8: 21.5 / 26.1;
+//   twelve rows a head (two products), 16/4 heads of 128:  one sequence  1: 8.4 / 9.3,  2: 9.3 / 8.6;  16 sequences  4: 11.8 / 10.8;  64 sequences  8: 17.0 / 19.9;
+//   60 new tokens, 12/4 heads of 64:  one sequence  3: 12.7 / 13.6,  4: 14.8 / 13.8;  16 sequences  4: 15.2 / 16.4.
+// A loop of calls from the host, which a launch more takes 2.2 us longer (10.7 -> 12.8 for one sequence at any of these lengths), is not what the rule goes by.
+inline bool whole_items(long long items, long long tiles, int ctas, int few, int most) { return tiles <= few || (tiles <= most && 4 * items >= ctas); }
 
 // What an item is.  runs(): the items of a sequence for one head; tiles(): the steps of work of run p, at least one, and where they
 // begin; uniform(): the steps where every run has the same number, else 0.
