@@ -3,8 +3,9 @@
 // Selection, one to eight blocks (a cluster) for a sequence and head: the `need`-th largest weight among the tokens that are neither sinks nor
 // recent, by a radix search over the weights' order-preserving integers (11, 11 and 10 bits: a histogram in every block's shared memory,
 // summed over the cluster, then the digit in which the count is reached), and then one pass in token order that writes the indices above
-// it and the first ones equal to it.  The weights are read once and stay in shared memory.  Bound by latency: three histograms and their sums
-// follow one another; clusters are as large as the GPU has room for and a block has 2048 tokens left.
+// it and the first ones equal to it.  The weights are read once and stay in shared memory, except where a block's part is longer than it holds (EV_HELD:
+// one block for each of 75 or more heads, beyond 40,960 tokens): then every pass reads them anew.  Bound by latency: three histograms and their
+// sums follow one another; clusters are as large as the GPU has room for and a block has 2048 tokens left.
 // 65,536 tokens x 8 heads: 120 -> 27 us against one block a head that reads its weights anew for every pass.
 // Move: bound by HBM.  A warp takes 32 kept tokens: its lanes look up where they lie and go, then all of them copy row after row, sixteen bytes a
 // lane, eight rows under way.
@@ -31,30 +32,28 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sums over the block's threads of two counts packed in one word (each below 2^31), and the total.
-__device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long* warp_sums, unsigned long long& total) {
+// Exclusive sums of counts over the block's threads.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned long long s = v;
+    uint32_t s = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long t = __shfl_up_sync(0xffffffffu, s, o);
+        const uint32_t t = __shfl_up_sync(0xffffffffu, s, o);
         if (lane >= o) s += t;
     }
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
     if (warp == 0) {
-        unsigned long long w = warp_sums[lane];
+        uint32_t w = warp_sums[lane];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long t = __shfl_up_sync(0xffffffffu, w, o);
+            const uint32_t t = __shfl_up_sync(0xffffffffu, w, o);
             if (lane >= o) w += t;
         }
         warp_sums[lane] = w;
     }
     __syncthreads();
-    const unsigned long long base = warp ? warp_sums[warp - 1] : 0ull;
-    total = warp_sums[31];
-    return base + s - v;
+    return (warp ? warp_sums[warp - 1] : 0u) + s - v;
 }
 
 // ---- clusters of blocks --------------------------------------------------------------------------------------------
@@ -85,7 +84,7 @@ __global__ void __launch_bounds__(EV_THREADS)
 evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
     extern __shared__ uint32_t ev_keys[];
     __shared__ __align__(16) uint32_t bins[2][EV_BINS];                // the largest digit first
-    __shared__ unsigned long long warp_sums[32];
+    __shared__ uint32_t warp_sums[32];
     __shared__ uint32_t found[3];                                      // the digit, how many are still wanted inside it, and how many it has
     __shared__ uint32_t larger_of[33], equal_of[33];                   // counts of the block's warps, then of the block
     const int blocks = (int)cluster_size(), rank = (int)cluster_rank();
@@ -174,8 +173,7 @@ evict_select_kernel(const __grid_constant__ EvictParams P, int held) {
                     }
             }
         }
-        unsigned long long total;
-        uint32_t above = (uint32_t)block_scan(q.x + q.y + q.z + q.w, warp_sums, total);
+        uint32_t above = block_scan(q.x + q.y + q.z + q.w, warp_sums);
         const uint32_t count_of[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {

@@ -97,3 +97,16 @@ def test_bad_pages_are_reported():
     before = cache.k[:12].clone()
     vt.vitint_cache_evict(cache, batch, w, 32, new)
     assert vt.vitint_device_status() == -1 and torch.equal(cache.k[:12], before)
+
+
+def test_parts_that_shared_memory_does_not_hold():
+    """More than 40,960 tokens a block: 75 sequence-heads have a block each, and what it does not hold is read anew in every pass."""
+    g = torch.Generator().manual_seed(12)
+    run(12, 64, 128, I8, 15, [45000, 41500, 7, 0, 300], 300, 4, 100, weigh=lambda s: torch.randint(0, 400, s, generator=g).float())
+    run(13, 64, 128, I8, 15, [100, 41111, 40960, 40961, 1], 35000, 0, 0)
+
+
+@pytest.mark.parametrize("heads,lengths", [(1, [8191]), (1, [8192]), (1, [16383]), (1, [20000]), (9, [8200]), (18, [9001]), (37, [6000]), (74, [4097])])
+def test_clusters_of_every_size(heads, lengths):
+    g = torch.Generator().manual_seed(13)
+    run(14, 64, 64, I8, heads, lengths, 1500, 3, 200, weigh=lambda s: torch.randint(0, 5000, s, generator=g) / 64)
