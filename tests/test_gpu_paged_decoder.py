@@ -88,3 +88,40 @@ def test_prompt_eviction_and_further_tokens(dtype):
     # three more tokens, one and two, over what is left; positions go on as if nothing had been taken out
     step(new_table, [41, 42], [1, 2], [151, 62, 63])
     step(new_table, [42, 43], [1, 1], [152, 64])
+
+
+def test_two_streams_side_by_side():
+    """Two calls at once, each with its own workspace, queries and outputs, over one cache: the same bits as one after the other."""
+    g = torch.Generator().manual_seed(2)
+    cache = vt.PagedCache.empty(PAGES, HK, PLACES, D)
+    cache.k.copy_(torch.randn(cache.k.shape, generator=g)), cache.v.copy_(torch.randn(cache.v.shape, generator=g))
+    table = torch.randperm(PAGES, generator=g).to(torch.int32).view(2, -1).cuda()
+    calls = []
+    for lengths, news in (([500, 200], [1, 1]), ([430, 512], [100, 37])):
+        starts = torch.tensor([0, news[0], sum(news)], dtype=torch.int32).cuda()
+        batch = vt.CacheBatch(table, torch.tensor(lengths, dtype=torch.int32).cuda(), starts, max(news), 512)
+        q = torch.randn(sum(news), HQ, D, generator=g).to(torch.bfloat16).cuda()
+        work = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (vt.vitint_paged_attention_workspace_bytes(HQ, cache, batch),
+                                                                            vt.vitint_cache_weigh_workspace_bytes(cache, batch))]
+        calls.append((q, batch, work, torch.empty_like(q), torch.empty(q.shape[:2], device="cuda"), torch.zeros(PAGES, HK, PLACES, device="cuda")))
+
+    def call(q, batch, work, out, lse, weights):
+        vt.vitint_paged_attention(q, cache, batch, 0.125, out=out, lse=lse, workspace=work[0])
+        vt.vitint_cache_weigh(q, lse, cache, batch, 0.125, None, weights, workspace=work[1])
+
+    want = []
+    for c in calls:
+        call(*c)
+        want.append([t.clone() for t in c[3:]])
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                for t in c[3:5]:
+                    t.zero_()
+                call(*c)
+    torch.cuda.synchronize()
+    for c, w in zip(calls, want):
+        assert all(torch.equal(a, b) for a, b in zip(c[3:], w))
+    assert vt.vitint_device_status() == 0

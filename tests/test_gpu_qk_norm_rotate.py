@@ -188,3 +188,32 @@ def test_one_token_of_rows_of_any_width():
     parts = [row[:, i:i + 128].contiguous() for i in (0, 128, 256)]
     q2, _ = vt.vitint_qk_norm_rotate(*parts, 128, q_gain=one, k_gain=one, cache=plain, slots=slot)
     assert torch.equal(q, q2) and torch.equal(k[0, 0], plain.k[0, 0, 5]) and torch.equal(given.k, plain.k) and torch.equal(given.v, plain.v)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_a_cache_with_places_outside_heads(codes):
+    g = torch.Generator().manual_seed(8)
+    x = torch.randn(30, 4 * 64, generator=g).to(BF16).cuda()
+    plain = vt.PagedCache.empty(3, 2, 16, 64, I8 if codes else BF16)
+    views = [torch.empty(3, 16, 2, 64, dtype=plain.k.dtype, device="cuda").transpose(1, 2) for _ in range(2)]
+    turned = vt.PagedCache(*views, *(None if s is None else torch.empty_like(s) for s in (plain.k_steps, plain.v_steps)))
+    slots, one = torch.randperm(48, generator=g)[:30].cuda(), torch.ones(64, device="cuda")
+    for c in (plain, turned):
+        for t in (c.k, c.v, c.k_steps, c.v_steps):
+            if t is not None:
+                t.fill_(3)
+        vt.vitint_qk_norm_rotate(None, x[:, :128], x[:, 128:], 64, k_gain=one, cache=c, slots=slots, out_dtype=BF16)
+    for name in ("k", "v") + (("k_steps", "v_steps") if codes else ()):
+        assert torch.equal(getattr(plain, name), getattr(turned, name)), name
+    assert not bool((plain.k == 3).all())
+
+
+def test_keys_alone_and_a_layer_norm_without_an_offset():
+    g = torch.Generator().manual_seed(9)
+    x, gain = torch.randn(33, 3 * 128, generator=g) + 0.5, torch.randn(128, generator=g)
+    positions, freq = torch.arange(33, dtype=torch.int32), 50.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64)
+    y, tol = definition(x.view(33, 3, 128), "layer", 1e-6, gain.double(), torch.zeros(128, dtype=torch.float64), positions, freq, True)
+    _, k = vt.vitint_qk_norm_rotate(None, x.cuda(), None, 128, norm="layer", k_gain=gain.cuda(), positions=positions.cuda(), frequencies=freq.cuda(), pairs=True,
+                                    out_dtype=F16)
+    off = (k.double().cpu() - y).abs()
+    assert bool((off <= EPS[F16] / 2 * (y.abs() + tol) + tol + 2.0 ** -25).all())
