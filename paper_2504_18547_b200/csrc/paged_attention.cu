@@ -136,7 +136,7 @@ __device__ __forceinline__ void write_product(const RowsParams& P, const Sequenc
         __syncwarp();
     }
 }
-// (m is lower than the maximum that l refers to by the offset)
+// (m is lower than the maximum that l refers to by the offset, and loses nothing when that is added again)
 template <int NQ>
 __device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s, int h, int p, const float (&m)[NQ][2], const float (&l)[NQ][2], float offset) {
     const int lane = threadIdx.x & 31, i0 = p * P.plan.tile_tokens, rows = min(P.plan.tile_tokens, s.queries - i0) * P.plan.group;
@@ -148,7 +148,7 @@ __device__ __forceinline__ void write_lse(const RowsParams& P, const Sequence& s
             const int row = 8 * n + 2 * lane + e;
             if (row >= rows) continue;
             const int i = row / P.plan.group, head = h * P.plan.group + row - i * P.plan.group;
-            P.lse[(long long)(s.first + i0 + i) * P.q_heads + head] = l[n][e] > 0.0f ? (m[n][e] + (log2f(l[n][e]) + offset)) * 0.69314718055994531f : -INFINITY;
+            P.lse[(long long)(s.first + i0 + i) * P.q_heads + head] = l[n][e] > 0.0f ? ((m[n][e] + offset) + log2f(l[n][e])) * 0.69314718055994531f : -INFINITY;
         }
 }
 

@@ -560,7 +560,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     part[D * 128] = m - OFFSET;
                     part[(D + 1) * 128] = l;
                 } else if (P.lse) {
-                    P.lse[token * P.q_heads + head] = l > 0.0f ? ((m - OFFSET) + (log2f(l) + OFFSET)) * 0.69314718055994531f : -INFINITY;
+                    P.lse[token * P.q_heads + head] = l > 0.0f ? (((m - OFFSET) + OFFSET) + log2f(l)) * 0.69314718055994531f : -INFINITY;
                 }
             }
             ptx::tc_fence_before();
@@ -624,7 +624,7 @@ paged_tiles_join_kernel(const __grid_constant__ TilesParams P) {
         for (int q = 0; q < 4; ++q) p[q] = pack16<T>(o[k + 2 * q] * inv, o[k + 2 * q + 1] * inv);
         *reinterpret_cast<uint4*>(to + k) = make_uint4(p[0], p[1], p[2], p[3]);
     }
-    if (P.lse && col0 == 0) P.lse[token * P.q_heads + head] = l > 0.0f ? (m + (log2f(l) + TILES_OFFSET<T, CODES>)) * 0.69314718055994531f : -INFINITY;
+    if (P.lse && col0 == 0) P.lse[token * P.q_heads + head] = l > 0.0f ? ((m + TILES_OFFSET<T, CODES>) + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
 inline size_t tiles_partial_bytes(int ctas, int head_dim) { return (size_t)ctas * 2 * 2 * (head_dim + 2) * 128 * 4; }

@@ -408,3 +408,21 @@ def test_strides_that_nothing_steps_by():
         _, lse = vt.vitint_paged_attention(qd, one_page, batch, 0.09, out=out, want_lse=True)
         pu.check_attention(out, lse, pu.attention64(q, cache, table, lengths, starts, 0.09, True, 0))
     assert vt.vitint_device_status() == 0
+
+
+@pytest.mark.parametrize("qtype,ctype", [(BF16, BF16), (F16, F16), (BF16, I8)])
+@pytest.mark.parametrize("new", [1, 20])
+def test_logarithms_of_equal_scores(new, qtype, ctype):
+    """Scores of zero: the logarithm of the number of keys, off by a unit in the last place of log2 and the roundings of two products (2^-22 of it),
+    and nothing that depends on what probabilities are taken relative to."""
+    lengths = [2, 3, 5, 7, 13, 50, 100, 1000, 9000]
+    table, pages = torch.zeros(len(lengths), 141, dtype=torch.int32), 1                  # (all sequences in one page of zeros)
+    shape = (pages, 1, 64, 64)
+    steps = [torch.ones(shape[:3])] * 2 if ctype == I8 else []
+    cache = pu.to_gpu(vt.PagedCache(torch.zeros(shape, dtype=ctype), torch.zeros(shape, dtype=ctype), *steps))
+    starts = (torch.arange(len(lengths) + 1) * new).to(torch.int32)
+    batch = vt.CacheBatch(table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts.cuda(), new, 9000)
+    _, lse = vt.vitint_paged_attention(torch.ones(len(lengths) * new, 1, 64, dtype=qtype, device="cuda"), cache, batch, 1.0, causal=False, want_lse=True)
+    want = torch.tensor(lengths, dtype=torch.float64).log().repeat_interleave(new)
+    off = (lse[:, 0].double().cpu() - want).abs()
+    assert bool((off <= 2.0 ** -22 * want).all()), off / want
