@@ -485,7 +485,7 @@ typedef struct {
     const int32_t* lengths;      /* device [sequences] */
     const int32_t* query_starts; /* device [sequences + 1] */
     int32_t sequences;
-    int32_t max_queries;         /* no sequence has more new tokens */
+    int32_t max_queries;         /* no sequence has more new tokens (a looser bound may select a kernel for more of them) */
     int64_t max_length;          /* no sequence is longer; at most table_stride * page_tokens and 2^29 */
 } vitint_cache_batch;
 
@@ -531,8 +531,12 @@ int vitint_qk_norm_rotate(const vitint_qk_norm_rotate_desc* d, const vitint_cach
 
 /* Attention of every sequence's new tokens over what the cache holds of it (Eq. 3 for new tokens).  Query i of a sequence with
  *   n new tokens and length L has position L - n + i; it sees key j < L where causal == 0, j <= position where causal == 1 and,
- *   with window > 0 (causal only), j > position - window.  Scores and the softmax's maximum and sum are fp32; probabilities
- *   enter the second contraction rounded to the queries' type.  A query that sees no key gives zeros and lse = -inf.
+ *   with window > 0 (causal only), j > position - window.  Scores and the softmax's maximum and sum are fp32.  Probabilities
+ *   enter the second contraction as bf16 over a bf16 cache, and as fp16 over a cache of fp16 values or codes (times the value's step, relative to
+ *   the largest step among the keys that some query of a tile sees); fp16 ones are taken with an offset, so that what is lost from the output lies
+ *   below 2^-29 of the maximum.  Up to eight query rows a head of the cache (max_queries times query heads that share it) two such numbers hold a probability,
+ *   so that its rounding does not show, except with bf16 queries over codes.  A query that sees no key gives zeros and lse = -inf.
+ *   scale: positive and finite.
  *   q: [tokens, q_heads, head_dim] of q_type (VITINT_BF16 or F16; the cache's type unless that is VITINT_I8), channel stride 1,
  *     16-byte aligned, strides multiples of 8 elements.  q_heads is a multiple of kv_heads: query head h reads
  *     head h / (q_heads / kv_heads); at most 128 query heads share one.  out: same type and rules.
@@ -541,7 +545,7 @@ int vitint_qk_norm_rotate(const vitint_qk_norm_rotate_desc* d, const vitint_cach
  *   are finite: a value that is not may reach queries that the mask keeps from it.
  *   workspace: device scratch, 256-byte aligned, >= vitint_paged_attention_workspace_bytes(); contents undefined after; two calls
  *     that may overlap (streams, graphs replayed side by side) need one each.
- *   A page index outside the cache reads as zeros, a length beyond max_length or page table counts as that bound, and query ranges
+ *   A page index outside the cache reads as zeros (codes: with steps of zero), a length beyond max_length or page table counts as that bound, and query ranges
  *     outside q are cut; each makes the next vitint_device_status() return VITINT_ERR_INVALID_ARG.
  *   Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA. */
 size_t vitint_paged_attention_workspace_bytes(int32_t q_heads, const vitint_cache* cache, const vitint_cache_batch* batch);
@@ -552,7 +556,7 @@ int vitint_paged_attention(const void* q, int32_t q_type, int64_t tokens, int32_
 
 /* The attention weight that cached tokens receive: for every token j of every sequence and every head of the cache
  *   weights_out[place of j] = weights_in[place of j] + sum over the new tokens i that see j and the query heads of the group
- *                             of exp(score_ij - lse_i)
+ *                             of exp(score_ij - lse_i)  (0 where that is below 2^-126)
  *   with the scores and the mask of vitint_paged_attention and the lse it returned.  Sums are fp32 in a fixed order.  Places that hold
  *   no token of the batch are left as they are.  Sequences share no pages.
  *   weights_in, weights_out: device fp32 [pages][kv_heads][page_tokens]; they may be the same array; weights_in NULL counts as zeros.

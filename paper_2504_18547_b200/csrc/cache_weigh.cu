@@ -6,8 +6,8 @@
 // For prompts it is bound by shared memory: the product of 128 x 128 scores reads 64 KB of operands, which is what shared memory delivers in its
 // 512 cycles, and every thread loads the rows' logarithms beside it (1023 tokens x 32 heads over 12,287 cached codes: 151 us, 660 TFLOP/s; without
 // these loads 121, with a quarter of the products 140; loading them once for two keys of a thread costs registers: 167).  The exponentials, 16 a clock
-// and SM, take 1024 cycles of the special-function unit; a part of them goes through the FMA pipe (all through the unit: 164 us).  For single tokens it
-// is bound by reading the keys.  Two tiles of keys stay in shared memory while the query tiles that see them stream past (one would have 32 KB
+// and SM, take 1024 cycles of the special-function unit; a part of them goes through the FMA pipe (all through the unit: 164 us).  Over 16-bit keys the same takes 134 us.  For single
+// tokens it is bound by reading the keys and by a tile's latency (32 sequences of up to 4096 tokens: 27 us for 18 of bytes; over codes 38).  Two tiles of keys stay in shared memory while the query tiles that see them stream past (one would have 32 KB
 // of queries come from L2 for every 128 x 128 scores); a group of four warps has the scores of one of them, in two buffers each.  Work is shared out
 // evenly as for the attention (paged_plan.cuh), with keys and queries in each other's places; a run of keys whose queries are split between CTAs is
 // summed by a second kernel in the CTAs' order.

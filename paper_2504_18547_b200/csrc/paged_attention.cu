@@ -12,10 +12,11 @@
 // 8-bit codes become fp16 operands in registers (exact): the order of the contraction's index is free as long as both sides agree, so a thread
 // takes its codes as they lie, sixteen bytes at a time.
 // Up to eight rows a probability is multiplied as the sum of two 16-bit numbers (the tensor core is idle otherwise), so that only the output is
-// rounded.
+// rounded.  With bf16 queries over codes it is one fp16 number: the output is rounded eight times as coarsely.
 //
-// One token each of 48 sequences with up to 8192 cached ones (32 query heads on 8 of 128, 680 MB): 115 us, 5.9 TB/s; 2 x 3 tokens over 131,072 (12
-// rows a head): 98 us, 5.5 TB/s; 64 sequences of codes (346 MB): 83 us, 4.2 TB/s (queries as rows, bf16 operands: 123).
+// One token each of 48 sequences with up to 8192 cached ones (32 query heads on 8 of 128, 680 MB): 116 us, 5.8 TB/s; 2 x 3 tokens over 131,072 (12
+// rows a head): 98 us, 5.5 TB/s; 64 sequences of codes (346 MB): 85 us, 4.1 TB/s (queries as rows, bf16 operands: 123), where the ALU, which expands the
+// codes, is busy for 57 % of the time and 59 % of the issue slots are taken.
 #include "paged_tiles.cuh"
 #include "paged_attention_tiles.cu"
 
@@ -38,7 +39,7 @@ struct RowsShape {
     static constexpr int STEPS = CODES ? KT * 4 : 0;                   // bytes of a tile's key (or value) steps
     static constexpr int STAGE = 2 * HALF;
     // CTAs on an SM, and tiles in a CTA's ring.  Codes are bound by latency as much as by bytes (they are half of them, and expanded): more CTAs
-    // with fewer tiles (64 sequences of up to 6001 tokens: three CTAs of four tiles 95 us, four of two 85).
+    // with fewer tiles (64 sequences of up to 6001 tokens: three CTAs of four tiles 95 us, four of two 85 at the time).
     static constexpr int CTAS = NQ == 2 ? 2 : CODES ? 4 : 3;
     static constexpr int STAGES = CODES ? (NQ == 2 ? 5 : 2) : (NQ == 2 ? 3 : 2);
     static constexpr int NREG = NQ * D / 4;                            // a thread's outputs

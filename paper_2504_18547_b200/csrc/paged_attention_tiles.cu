@@ -11,7 +11,8 @@
 // codes are expanded to 16-bit operands by four more warps (exact), their steps multiply scores and probabilities.
 // Work is shared out evenly over one CTA an SM (paged_plan.cuh); items split between CTAs are joined by a second kernel.
 //
-// 2048 tokens over 18,432 (32 query heads on 8 of 128): 503 us in a burst (1160 TFLOP/s), 613 in a long loop under the power cap.  A half's
+// 2048 tokens over 18,432 (32 query heads on 8 of 128): 503 - 530 us in a burst (1110 - 1160 TFLOP/s), 615 in a long loop under the power cap; over codes
+// 1102 us in a burst (530 TFLOP/s).  A half's
 // probabilities (1.2 us) and its two products (0.9 us until the next scores are there, 0.55 of it work) follow one another, as the next scores take the
 // columns of the probabilities: with two halves the tensor core is busy for three quarters of the time.  Several chunks of up to 701 tokens with a
 // window (12 heads on 4 of 64): 39 us, ten tiles a CTA, where the plan (2 us), changes of items (2 to 4 us each) and the join (6 us) count as much.
