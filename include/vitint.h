@@ -480,7 +480,8 @@ typedef struct {
  *   query_starts[b] .. query_starts[b+1]: the rows of q that are the last tokens of sequence b (ascending, from row 0 on;
  *     an empty range is allowed).  Rows behind query_starts[sequences] belong to no sequence and are left as they are. */
 typedef struct {
-    const int32_t* page_table;   /* device [sequences][table_stride]; entries behind a sequence's last page are not read */
+    const int32_t* page_table;   /* device [sequences][table_stride]; entries behind a sequence's last page are not read, those
+                                  * in front of a window are */
     int64_t table_stride;        /* entries of a row */
     const int32_t* lengths;      /* device [sequences] */
     const int32_t* query_starts; /* device [sequences + 1] */

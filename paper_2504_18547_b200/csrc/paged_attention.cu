@@ -39,7 +39,7 @@ struct RowsShape {
     static constexpr int STEPS = CODES ? KT * 4 : 0;                   // bytes of a tile's key (or value) steps
     static constexpr int STAGE = 2 * HALF;
     // CTAs on an SM, and tiles in a CTA's ring.  Codes are bound by latency as much as by bytes (they are half of them, and expanded): more CTAs
-    // with fewer tiles (64 sequences of up to 6001 tokens: three CTAs of four tiles 95 us, four of two 85 at the time).
+    // with fewer tiles (64 sequences of up to 6001 tokens: three CTAs of four tiles 95 us, four of two 85).
     static constexpr int CTAS = NQ == 2 ? 2 : CODES ? 4 : 3;
     static constexpr int STAGES = CODES ? (NQ == 2 ? 5 : 2) : (NQ == 2 ? 3 : 2);
     static constexpr int NREG = NQ * D / 4;                            // a thread's outputs

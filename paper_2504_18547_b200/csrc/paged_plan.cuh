@@ -5,8 +5,8 @@
 // sequence by sequence, head by head, run by run, form one line, and every CTA takes an equal stretch of it: whatever the lengths are, no CTA
 // has more than one tile above the mean.  A stretch that ends inside an item leaves a partial result (row maxima, sums and unnormalised outputs)
 // in the workspace, at most two a CTA, and a second kernel joins them.  Short items stay whole (whole_items): a CTA then has all tiles of the items
-// that begin in its stretch, up to an item's less one above its share.  The plan is made on the device from the lengths, so a recorded graph may be replayed with others; it is a
-// warp's work: lanes take sequences, or the runs of one long chunk.
+// that begin in its stretch, up to an item's less one above its share.  The plan is made on the device from the lengths, so a
+// recorded graph may be replayed with others; it is a warp's work: lanes take sequences, or the runs of one long chunk.
 #pragma once
 
 #include "cache.cuh"
@@ -20,14 +20,16 @@ struct PlanParams {
     int whole;                            // items are not split: a CTA has those that begin in its stretch
 };
 
-// Whether items stay whole: a second launch to join parts costs about 1.5 us on the device (and 2.2 us of the host).  That is more than what splitting gains where
-// the longest item has at most `few` tiles, and up to `most` tiles where the items alone fill a quarter of the grid.  Recorded calls, us whole / split:
-//   one token, 12 heads of 64, tiles of 128 keys, one sequence:  3 tiles 7.1 / 7.4,  4: 7.9 / 7.5,  7: 10.1 / 7.4;  16 sequences:  4: 9.2 / 10.6,  7: 12.3 / 13.2;
-//   one token, 32/8 heads of 128, tiles of 64:  one sequence  3: 7.4 / 7.7,  6: 9.1 / 7.7;  8 sequences  6: 10.2 / 9.9;  16 sequences  6: 11.0 / 11.2;
-//   the same over codes (a grid a third larger):  one sequence  2: 7.7 / 8.2,  4: 9.5 / 8.4;  16 sequences  4: 12.4 / 11.4,  8: 18.0 / 13.2;  64 sequences  8: 21.5 / 26.1;
-//   twelve rows a head (two products), 16/4 heads of 128:  one sequence  1: 8.4 / 9.3,  2: 9.3 / 8.6;  16 sequences  4: 11.8 / 10.8;  64 sequences  8: 17.0 / 19.9;
-//   60 new tokens, 12/4 heads of 64:  one sequence  3: 12.7 / 13.6,  4: 14.8 / 13.8;  16 sequences  4: 15.2 / 16.4.
-// A loop of calls from the host, which a launch more takes 2.2 us longer (10.7 -> 12.8 for one sequence at any of these lengths), is not what the rule goes by.
+// Whether items stay whole: a second launch to join parts costs about 1.5 us on the device (and 2.2 us of the host).  That is more than what splitting
+// gains where the longest item has at most `few` tiles, and up to `most` tiles where the items alone fill a quarter of the grid.  Recorded calls,
+// us whole / split:
+//   one token, 12 heads of 64, tiles of 128 keys:    1 sequence   3 tiles 7.1 / 7.4,  4: 7.9 / 7.5,  7: 10.1 / 7.4;  16 sequences  4: 9.2 / 10.6,  7: 12.3 / 13.2
+//   one token, 32/8 heads of 128, tiles of 64:       1 sequence   3: 7.4 / 7.7,  6: 9.1 / 7.7;  8 sequences  4: 8.9 / 9.6,  6: 10.2 / 9.9;  16  6: 11.0 / 11.2
+//   the same over codes (a grid a third larger):     1 sequence   2: 7.7 / 8.2,  4: 9.5 / 8.4;  16 sequences  4: 12.4 / 11.4,  8: 18.0 / 13.2;  64  8: 21.5 / 26.1
+//   twelve rows a head (two products), 16/4 of 128:  1 sequence   1: 8.4 / 9.3,  2: 9.3 / 8.6;  16 sequences  4: 11.8 / 10.8;  64  8: 17.0 / 19.9
+//   60 new tokens, 12/4 heads of 64:                 1 sequence   3: 12.7 / 13.6,  4: 14.8 / 13.8;  16 sequences  4: 15.2 / 16.4
+// A loop of calls from the host, which a launch more takes 2.2 us longer (10.7 -> 12.8 for one sequence at any of these lengths), is not what the rule
+// goes by.
 inline bool whole_items(long long items, long long tiles, int ctas, int few, int most) { return tiles <= few || (tiles <= most && 4 * items >= ctas); }
 
 // What an item is.  runs(): the items of a sequence for one head; tiles(): the steps of work of run p, at least one, and where they
