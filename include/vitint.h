@@ -559,7 +559,8 @@ int vitint_paged_attention(const void* q, int32_t q_type, int64_t tokens, int32_
  *   weights_out[place of j] = weights_in[place of j] + sum over the new tokens i that see j and the query heads of the group
  *                             of exp(score_ij - lse_i)  (0 where that is below 2^-126)
  *   with the scores and the mask of vitint_paged_attention and the lse it returned.  Sums are fp32 in a fixed order.  Places that hold
- *   no token of the batch are left as they are.  Sequences share no pages.
+ *   no token of the batch are left as they are.  Sequences share no pages: places of a page that two of them name would receive
+ *   the one's weights or the other's, not both.
  *   weights_in, weights_out: device fp32 [pages][kv_heads][page_tokens]; they may be the same array; weights_in NULL counts as zeros.
  *   workspace: as for vitint_paged_attention, >= vitint_cache_weigh_workspace_bytes() bytes.
  *   Other arguments, rules and errors as vitint_paged_attention. */
